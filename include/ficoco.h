@@ -70,7 +70,8 @@ enum ficoco_error {
   FICOCO_ERR_TIMEOUT = -6,       /* a bounded device-side wait ran out */
   FICOCO_ERR_CAPTURE = -7,       /* a new plan would have to be uploaded during stream capture */
   FICOCO_ERR_GRID = -8,          /* grid_h * grid_w smaller than the number of alive patches */
-  FICOCO_ERR_STATIC_LIMIT = -9   /* problem larger than the fixed scratch of the allocation-free entry point */
+  FICOCO_ERR_STATIC_LIMIT = -9,  /* problem larger than the fixed scratch of the allocation-free entry point */
+  FICOCO_ERR_PAGES = -10         /* a pool has too few free pages, or a page is not held */
 };
 
 enum ficoco_flags {
@@ -273,7 +274,8 @@ int ficoco_l_reduce_host(ficoco_ctx* ctx, const ficoco_l_args* host_args,
  * bit 2 (4): a bounded device-side wait ran out: the outputs of that step and of every step
  * enqueued after it are invalid; bit 3 (8): an internal index list held a token index outside
  * its image, which was replaced by 0 instead of being followed: the outputs of that step are
- * invalid).  Returns FICOCO_OK when the word could be read, whatever it holds. */
+ * invalid; bit 4 (16): a cache call met a page, length, row offset or kept index out of range, see the 8-bit cache below).
+ * Returns FICOCO_OK when the word could be read, whatever it holds. */
 int ficoco_status(ficoco_ctx* ctx, void* cuda_stream, int* device_status);
 
 /* Testing hook for the bounded waits.  wait_ns > 0 sets the time after which a device-side wait
@@ -379,6 +381,143 @@ int ficoco_equivalent_token(const void* keys, int dtype, int batch, int n_tokens
 #define FICOCO_NOALLOC_MAX_DIM 2048
 int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, int n_tokens, int dim,
                                      unsigned flags, float* v_out, void* cuda_stream);
+
+/*
+ * 8-bit paged key/value cache of a decoder layer, next to ficoco_l_reduce.
+ *
+ * Keys and values lie in pages of `page_size` tokens as e4m3 codes (finite values up to 448) with one fp32 scale for
+ * each page and key/value head: value = code * scale.  A scale is a power of two, the smallest 2^e >= 2^-64 with
+ * (largest magnitude of the page and head) <= 448 * 2^e, so that a division by it is exact and codes are rescaled
+ * without another rounding unless they leave e4m3's normal range.
+ *
+ * Sequence b has lengths[b] tokens; token j lies in slot j % page_size of page page_table[b * table_stride +
+ * j / page_size].  Entries beyond a sequence's last page are never read.  Lengths and tables are device memory and are read
+ * by the kernels, so that a captured graph follows them.  `lengths` counts the tokens of the same step: a caller raises it by
+ * the new rows first, then appends and attends with the same numbers.
+ *
+ * The rows of a call are packed, sequence after sequence: sequence b has rows cu_rows[b] .. cu_rows[b + 1] - 1, and they
+ * are the LAST tokens of the sequence, at positions lengths[b] - n .. lengths[b] - 1.  Rows behind cu_rows[batch] are
+ * neither read nor written (a padded batch).
+ *
+ * What only the device can see sets bit 4 (16) of the status word: a page index outside the pool (replaced by 0 where it is
+ * read, skipped where it would be written), a length beyond max_pages * page_size or below zero (cut), a row offset outside
+ * the rows of the call (those rows are skipped), a kept index outside its sequence (replaced by 0).
+ *
+ * Supported: page_size 16, 32, 64 or 128; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
+ * multiple of kv_heads (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a
+ * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned.  Anything else returns
+ * FICOCO_ERR_INVALID_ARG or FICOCO_ERR_UNSUPPORTED and launches nothing.
+ *
+ * The first attention call of a context allocates its scratch (about 5 MB, never moved afterwards) and must therefore happen outside
+ * stream capture (FICOCO_ERR_CAPTURE).  Graphs captured from one context share that scratch: they must not run at the same time.
+ */
+typedef struct ficoco_cache {
+  void* k_codes;           /* device e4m3 [n_pages, kv_heads, page_size, head_dim] */
+  void* v_codes;
+  float* k_scale;          /* device fp32 [n_pages, kv_heads] */
+  float* v_scale;
+  const int* page_table;   /* device int32 [batch, max_pages], rows table_stride apart */
+  const int* lengths;      /* device int32 [batch] */
+  long long table_stride;
+  int n_pages;
+  int page_size;
+  int kv_heads;
+  int head_dim;
+  int batch;
+  int max_pages;
+} ficoco_cache;
+
+/*
+ * Writes the rows k, v [rows, kv_heads, head_dim] into the pages.  A page whose slot 0 is written gets its scale from
+ * the new rows alone (what it held before is gone); a page that holds older tokens of the sequence keeps its scale or, where
+ * the new rows need a larger one, has its codes rescaled to it (round to nearest, ties to even).  Slots behind a sequence's
+ * last token stay as they are.  A key or value row of a head that holds a NaN or an infinity is stored as a NaN key and a zero
+ * value and does not count for the scale: a query that sees the token gets NaN, every other one is untouched.
+ */
+typedef struct ficoco_append_args {
+  const void* k;           /* device, dtype, [rows, kv_heads, head_dim], rows k_stride elements apart */
+  const void* v;
+  const int* cu_rows;      /* device int32 [batch + 1] */
+  long long k_stride;
+  long long v_stride;
+  int dtype;               /* ficoco_dtype */
+  int rows;                /* rows of k and v, padding included */
+} ficoco_append_args;
+int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_append_args* args, void* cuda_stream);
+
+/*
+ * Attention of the rows q [rows, heads, head_dim] over the cache: out_i = sum_j p_ij v_j, p the softmax of
+ * scale * q_i . k_j over the tokens j that row i sees.  With position pos_i of row i, token j is seen if
+ * j < lengths[b], and with FICOCO_CAUSAL j <= pos_i, and with window > 0 j > pos_i - window or j < sinks.  A row that
+ * sees nothing gets zeros (lse -infinity).  lse (or NULL) receives the natural logarithm of the softmax's denominator.
+ * Codes are used as they are; a query row and the softmax weights are split into e4m3 terms (two for bf16 rows, the weights then
+ * exact to 2^-8, six for fp32), products are exact and summed in fp32.  Value codes must not be NaN (append writes none).
+ * out must not overlap q.
+ */
+enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };
+typedef struct ficoco_attention_args {
+  const void* q;           /* device, dtype, [rows, heads, head_dim], rows q_stride elements apart */
+  const int* cu_rows;      /* device int32 [batch + 1] */
+  void* out;               /* device, dtype, [rows, heads, head_dim] contiguous */
+  float* lse;              /* device fp32 [rows, heads]; read by ficoco_cache_weights, an output (or NULL) of ficoco_cache_attention */
+  long long q_stride;
+  float scale;             /* > 0 */
+  int dtype;
+  int rows;                /* rows of q, padding included */
+  int heads;
+  int window;              /* 0: none */
+  int sinks;               /* >= 0, used with a window */
+  unsigned flags;          /* ficoco_attention_flags */
+} ficoco_attention_args;
+int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_attention_args* args, void* cuda_stream);
+
+/*
+ * The attention weights of the last n_text rows of every sequence over the `count` tokens from `first` on, fp32
+ * [batch, heads, n_text, count]: what ficoco_l_reduce takes as attn_t2v.  args: those of the attention call before it, lse
+ * being its result (out is not used).  A token that a row does not see, a token behind the sequence's end and a row that the
+ * sequence does not have weigh 0.
+ */
+int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_attention_args* args, int n_text,
+                         int first, int count, float* weights, void* cuda_stream);
+
+/* Copies page src[i] to page dst[i] (device int32 [n]), codes and scales, for every i with src[i] and dst[i] >= 0.  A page
+ * must not occur twice in dst, nor in both lists. */
+int ficoco_cache_copy(ficoco_ctx* ctx, const ficoco_cache* cache, const int* src, const int* dst, int n, void* cuda_stream);
+
+/*
+ * Gathers the tokens that a reduce step has kept into other pages.  Sequence b becomes its first min(first, lengths[b]) tokens
+ * followed by tokens first + kept[i], i in cu_kept[b] .. cu_kept[b + 1] - 1 (ficoco_l_reduce's kept_idx where the reduced
+ * rows start at token `first` of the sequence), in that order.  Pages to_table[b * to_stride + ..] receive them, with
+ * scales of their own and codes rounded anew; they must not occur in the cache's page table, nor twice.  lengths_out
+ * (device int32 [batch], or NULL) receives the new lengths.
+ */
+typedef struct ficoco_compact_args {
+  const int* to_table;     /* device int32 [batch, to_pages], rows to_stride apart; not the cache's page_table */
+  const int* kept;         /* device int32 [n_kept] */
+  const int* cu_kept;      /* device int32 [batch + 1] */
+  int* lengths_out;
+  long long to_stride;
+  int to_pages;
+  int n_kept;              /* entries of kept, padding included */
+  int first;
+  int reserved;
+} ficoco_compact_args;
+int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_compact_args* args, void* cuda_stream);
+
+/*
+ * Page bookkeeping on the host: which pages of a pool are free, and how many sequences hold each of the others.  Not
+ * synchronised with the device: a page given back must not be handed out again before the kernels that read it are enqueued.
+ * Calls on one pool are not thread-safe.  FICOCO_ERR_PAGES: not enough free pages, nothing was taken.
+ */
+typedef struct ficoco_pool ficoco_pool;
+int ficoco_pool_create(ficoco_pool** out, int n_pages);
+int ficoco_pool_destroy(ficoco_pool* pool);
+int ficoco_pool_free_pages(const ficoco_pool* pool);
+int ficoco_pool_take(ficoco_pool* pool, int n, int* pages);            /* n free pages, lowest first, each held once */
+int ficoco_pool_give(ficoco_pool* pool, int n, const int* pages);      /* one holder less; free when none is left */
+/* Forks a sequence of `length` tokens: `forked` receives its page list, full pages shared (one holder more), a last page that is
+ * partly filled replaced by a new page; *copy_from / *copy_to receive that pair for ficoco_cache_copy (-1, -1 if there is none). */
+int ficoco_pool_fork(ficoco_pool* pool, int page_size, int length, const int* pages, int* forked, int* copy_from, int* copy_to);
 
 #ifdef __cplusplus
 }

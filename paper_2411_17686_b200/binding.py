@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libficoco.so")
 
 FICOCO_FP32, FICOCO_BF16 = 0, 1
 FICOCO_HAS_CLS, FICOCO_LOCAL_PENALTY, FICOCO_AVERAGE_COMPRESSION, FICOCO_BACK_TO_BACK, FICOCO_CONVERGENT = 1, 2, 4, 8, 16
+FICOCO_CAUSAL = 1
 KCAP = 16
 
 INSPECT = {
@@ -34,6 +35,9 @@ EXPORTS = [
     "ficoco_profile", "ficoco_profile_read", "ficoco_vision_redundancy_noalloc",
     "ficoco_equivalent_token", "ficoco_v_reduce_relation", "ficoco_debug_waits", "ficoco_v_reduce_schedule",
     "ficoco_v_plan", "ficoco_debug_barrier_wait",
+    "ficoco_cache_append", "ficoco_cache_attention", "ficoco_cache_weights", "ficoco_cache_copy", "ficoco_cache_compact",
+    "ficoco_pool_create", "ficoco_pool_destroy", "ficoco_pool_free_pages", "ficoco_pool_take", "ficoco_pool_give",
+    "ficoco_pool_fork",
 ]
 
 
@@ -58,6 +62,30 @@ class ficoco_l_args(C.Structure):
                 ("out_tokens", C.c_void_p), ("kept_idx", C.c_void_p), ("scores_out", C.c_void_p),
                 ("dtype", C.c_int), ("batch", C.c_int), ("n_vision", C.c_int), ("n_text", C.c_int),
                 ("dim", C.c_int), ("heads", C.c_int), ("n_keep", C.c_int), ("reserved", C.c_int)]
+
+
+class ficoco_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_table", C.c_void_p), ("lengths", C.c_void_p), ("table_stride", C.c_longlong),
+                ("n_pages", C.c_int), ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("batch", C.c_int), ("max_pages", C.c_int)]
+
+
+class ficoco_append_args(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cu_rows", C.c_void_p), ("k_stride", C.c_longlong),
+                ("v_stride", C.c_longlong), ("dtype", C.c_int), ("rows", C.c_int)]
+
+
+class ficoco_attention_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("cu_rows", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("q_stride", C.c_longlong), ("scale", C.c_float), ("dtype", C.c_int), ("rows", C.c_int),
+                ("heads", C.c_int), ("window", C.c_int), ("sinks", C.c_int), ("flags", C.c_uint)]
+
+
+class ficoco_compact_args(C.Structure):
+    _fields_ = [("to_table", C.c_void_p), ("kept", C.c_void_p), ("cu_kept", C.c_void_p), ("lengths_out", C.c_void_p),
+                ("to_stride", C.c_longlong), ("to_pages", C.c_int), ("n_kept", C.c_int), ("first", C.c_int),
+                ("reserved", C.c_int)]
 
 
 class FicocoError(RuntimeError):
@@ -107,6 +135,19 @@ def load_library() -> C.CDLL:
                                         C.POINTER(C.c_longlong)]
     lib.ficoco_vision_redundancy_noalloc.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_uint,
                                                      C.c_void_p, C.c_void_p]
+    lib.ficoco_cache_append.argtypes = [C.c_void_p, C.POINTER(ficoco_cache), C.POINTER(ficoco_append_args), C.c_void_p]
+    lib.ficoco_cache_attention.argtypes = [C.c_void_p, C.POINTER(ficoco_cache), C.POINTER(ficoco_attention_args), C.c_void_p]
+    lib.ficoco_cache_weights.argtypes = [C.c_void_p, C.POINTER(ficoco_cache), C.POINTER(ficoco_attention_args), C.c_int,
+                                         C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+    lib.ficoco_cache_copy.argtypes = [C.c_void_p, C.POINTER(ficoco_cache), C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]
+    lib.ficoco_cache_compact.argtypes = [C.c_void_p, C.POINTER(ficoco_cache), C.POINTER(ficoco_compact_args), C.c_void_p]
+    lib.ficoco_pool_create.argtypes = [C.POINTER(C.c_void_p), C.c_int]
+    lib.ficoco_pool_destroy.argtypes = [C.c_void_p]
+    lib.ficoco_pool_free_pages.argtypes = [C.c_void_p]
+    lib.ficoco_pool_take.argtypes = [C.c_void_p, C.c_int, C.c_void_p]
+    lib.ficoco_pool_give.argtypes = [C.c_void_p, C.c_int, C.c_void_p]
+    lib.ficoco_pool_fork.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.POINTER(C.c_int),
+                                     C.POINTER(C.c_int)]
     _lib = lib
     return lib
 
@@ -193,6 +234,122 @@ class VResult:
     pos_out: "object"
     scores: "object"
     out_rows: List[int]   # output rows per image
+
+
+class PagedCache:
+    """The 8-bit paged key/value cache of one decoder layer: tensors that the caller owns, described once.
+
+    ``k_codes`` / ``v_codes``: cuda float8_e4m3fn (or uint8) [n_pages, kv_heads, page_size, head_dim];
+    ``k_scale`` / ``v_scale``: cuda fp32 [n_pages, kv_heads]; ``page_table``: cuda int32 [batch, max_pages] (rows may be
+    strided); ``lengths``: cuda int32 [batch].  Their contents may change between calls, the tensors may not: a cache with other
+    tensors is another ``PagedCache``."""
+
+    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "page_table", "lengths", "struct", "device")
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, lengths):
+        import torch
+        self.device = k_codes.device
+        n_pages, kv_heads, page_size, head_dim = k_codes.shape
+        for name, t, dtypes, shape in (
+                ("k_codes", k_codes, (torch.float8_e4m3fn, torch.uint8), (n_pages, kv_heads, page_size, head_dim)),
+                ("v_codes", v_codes, (torch.float8_e4m3fn, torch.uint8), (n_pages, kv_heads, page_size, head_dim)),
+                ("k_scale", k_scale, (torch.float32,), (n_pages, kv_heads)),
+                ("v_scale", v_scale, (torch.float32,), (n_pages, kv_heads)),
+                ("page_table", page_table, (torch.int32,), (page_table.shape[0], page_table.shape[-1])),
+                ("lengths", lengths, (torch.int32,), (page_table.shape[0],))):
+            if t.dtype not in dtypes:
+                raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+            if t.device != self.device or not t.is_cuda:
+                raise ValueError(f"{name} must be on the cuda device of k_codes, got {t.device}")
+            if not (t.stride(-1) == 1 if name == "page_table" else t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.page_table, self.lengths = page_table, lengths
+        self.struct = ficoco_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                   page_table.data_ptr(), lengths.data_ptr(), page_table.stride(0), n_pages, page_size,
+                                   kv_heads, head_dim, page_table.shape[0], page_table.shape[1])
+
+    @classmethod
+    def empty(cls, n_pages: int, kv_heads: int, page_size: int, head_dim: int, batch: int, max_pages: int,
+              device="cuda:0") -> "PagedCache":
+        """A cache of ``batch`` sequences without tokens."""
+        import torch
+        codes = [torch.zeros((n_pages, kv_heads, page_size, head_dim), dtype=torch.uint8, device=device)
+                 .view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.ones((n_pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(codes[0], codes[1], scales[0], scales[1],
+                   torch.zeros((batch, max_pages), dtype=torch.int32, device=device),
+                   torch.zeros((batch,), dtype=torch.int32, device=device))
+
+    @property
+    def batch(self) -> int:
+        return self.struct.batch
+
+
+class PagePool:
+    """Which pages of a cache are free, and how many sequences hold each of the others (host bookkeeping, ficoco_pool_*)."""
+
+    def __init__(self, n_pages: int):
+        self.lib = load_library()
+        h = C.c_void_p()
+        _check(None, self.lib.ficoco_pool_create(C.byref(h), n_pages))
+        self.h = h
+
+    def close(self) -> None:
+        if getattr(self, "h", None):
+            self.lib.ficoco_pool_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def free_pages(self) -> int:
+        return int(self.lib.ficoco_pool_free_pages(self.h))
+
+    def take(self, n: int) -> List[int]:
+        a = np.zeros(max(n, 1), dtype=np.int32)
+        _check(None, self.lib.ficoco_pool_take(self.h, n, a.ctypes.data))
+        return a[:n].tolist()
+
+    def give(self, pages: Sequence[int]) -> None:
+        a = np.ascontiguousarray(np.asarray(pages, dtype=np.int32))
+        _check(None, self.lib.ficoco_pool_give(self.h, a.shape[0], a.ctypes.data))
+
+    def fork(self, pages: Sequence[int], page_size: int, length: int) -> Tuple[List[int], Optional[Tuple[int, int]]]:
+        """The forked sequence's pages, and the (from, to) pair to copy with ``ficoco_cache_copy`` (None: nothing to copy)."""
+        n = -(-length // page_size) if page_size > 0 else 0
+        a = np.ascontiguousarray(np.asarray(pages, dtype=np.int32))
+        if a.shape[0] < n:
+            raise ValueError(f"{length} tokens need {n} pages, got {a.shape[0]}")
+        out = np.zeros(max(n, 1), dtype=np.int32)
+        src, dst = C.c_int(-1), C.c_int(-1)
+        _check(None, self.lib.ficoco_pool_fork(self.h, page_size, length, a.ctypes.data, out.ctypes.data, C.byref(src),
+                                               C.byref(dst)))
+        return out[:n].tolist(), (None if src.value < 0 else (src.value, dst.value))
+
+
+def _int32(name: str, t, n: Optional[int] = None) -> int:
+    """Address of a contiguous cuda int32 tensor."""
+    import torch
+    if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous cuda int32 tensor" + (f" of {n} values" if n is not None else ""))
+    return t.data_ptr()
+
+
+def _rows3(name: str, t, dim: int) -> int:
+    """Row stride of [rows, heads, dim] whose last two dimensions are contiguous."""
+    if t.dim() != 3 or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [rows, heads, {dim}], got {tuple(t.shape)}")
+    stride = t.stride()
+    if not t.is_cuda or (t.shape[0] > 0 and (stride[2] != 1 or (stride[1] != dim and t.shape[1] > 1))):
+        raise ValueError(f"{name} must be a cuda tensor with contiguous heads")
+    return stride[0] if t.shape[0] > 1 else t.shape[1] * dim
 
 
 class Context:
@@ -428,6 +585,98 @@ class Context:
         a.dim, a.heads, a.n_keep = dim, heads, n_keep
         _check(self.h, self.lib.ficoco_l_reduce_host(self.h, C.byref(a), C.byref(p)))
         return VResult(out_tokens, kept_idx, None, scores_out, out_rows)
+
+    # -- 8-bit paged cache --------------------------------------------------------------------
+    def ficoco_cache_append(self, cache: PagedCache, k, v, cu_rows, *, stream: Optional[int] = None) -> None:
+        """Writes k, v (cuda [rows, kv_heads, head_dim], bf16 or fp32, rows may be strided) as the last tokens of the
+        sequences; cu_rows: cuda int32 [batch + 1].  ``cache.lengths`` already counts them."""
+        cs = cache.struct
+        if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (cs.kv_heads, cs.head_dim):
+            raise ValueError(f"k and v must both be [rows, {cs.kv_heads}, {cs.head_dim}] of one type")
+        a = ficoco_append_args(k.data_ptr(), v.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1),
+                               _rows3("k", k, cs.head_dim), _rows3("v", v, cs.head_dim), _dtype_code(k), k.shape[0])
+        rc = self.lib.ficoco_cache_append(self.h, cs, a, _current_stream(cache.device) if stream is None else stream)
+        if rc:
+            _check(self.h, rc)
+
+    def _attention_args(self, cache, q, cu_rows, scale, causal, window, sinks) -> ficoco_attention_args:
+        cs = cache.struct
+        stride = _rows3("q", q, cs.head_dim)
+        return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1), None, None, stride,
+                                     cs.head_dim ** -0.5 if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
+                                     window, sinks, FICOCO_CAUSAL if causal else 0)
+
+    def ficoco_cache_attention(self, cache: PagedCache, q, cu_rows, *, scale: Optional[float] = None, causal: bool = True,
+                               window: int = 0, sinks: int = 0, out=None, lse=None, want_lse: bool = False,
+                               stream: Optional[int] = None):
+        """Attention of q (cuda [rows, heads, head_dim], the last tokens of the sequences) over the cache.  Returns out, or
+        (out, lse) with want_lse.  scale: 1 / sqrt(head_dim) by default; window / sinks: a row sees the last ``window`` tokens up to
+        its own and the first ``sinks``."""
+        import torch
+        a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+            raise ValueError("out must be contiguous, with q's shape and type")
+        if lse is None:
+            if want_lse:
+                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous fp32 [rows, heads]")
+        a.out = out.data_ptr()
+        if lse is not None:
+            a.lse = lse.data_ptr()
+        rc = self.lib.ficoco_cache_attention(self.h, cache.struct, a, _current_stream(cache.device) if stream is None else stream)
+        if rc:
+            _check(self.h, rc)
+        return (out, lse) if want_lse else out
+
+    def ficoco_cache_weights(self, cache: PagedCache, q, lse, cu_rows, n_text: int, first: int, count: int, *,
+                             scale: Optional[float] = None, causal: bool = True, window: int = 0, sinks: int = 0, out=None,
+                             stream: Optional[int] = None):
+        """fp32 [batch, heads, n_text, count]: what the last n_text rows of every sequence give the ``count`` tokens from
+        ``first`` on.  q, cu_rows and the mask are those of the attention call that returned lse; the result is ``attn_t2v`` of
+        ``ficoco_l_reduce``."""
+        import torch
+        a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
+        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous fp32 [rows, heads]")
+        shape = (cache.struct.batch, q.shape[1], n_text, count)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=q.device)
+        elif tuple(out.shape) != shape or out.dtype != torch.float32 or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous fp32 {shape}")
+        a.lse = lse.data_ptr()
+        rc = self.lib.ficoco_cache_weights(self.h, cache.struct, a, n_text, first, count, out.data_ptr(),
+                                           _current_stream(cache.device) if stream is None else stream)
+        if rc:
+            _check(self.h, rc)
+        return out
+
+    def ficoco_cache_copy(self, cache: PagedCache, src, dst, *, stream: Optional[int] = None) -> None:
+        """Copies page src[i] to page dst[i] (cuda int32 tensors of one length; pairs with a negative page are skipped)."""
+        rc = self.lib.ficoco_cache_copy(self.h, cache.struct, _int32("src", src), _int32("dst", dst, src.numel()), src.numel(),
+                                        _current_stream(cache.device) if stream is None else stream)
+        if rc:
+            _check(self.h, rc)
+
+    def ficoco_cache_compact(self, cache: PagedCache, to_table, kept, cu_kept, *, first: int = 0, lengths=None,
+                             stream: Optional[int] = None):
+        """Gathers the first ``first`` tokens of every sequence and its tokens first + kept[i] into the pages of ``to_table``
+        (cuda int32 [batch, pages], other pages than the cache's).  Returns the new lengths (cuda int32 [batch])."""
+        import torch
+        cs = cache.struct
+        if to_table.dtype != torch.int32 or to_table.dim() != 2 or to_table.shape[0] != cs.batch or not to_table.is_cuda or \
+                to_table.stride(1) != 1:
+            raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")
+        if lengths is None:
+            lengths = torch.empty((cs.batch,), dtype=torch.int32, device=to_table.device)
+        a = ficoco_compact_args(to_table.data_ptr(), _int32("kept", kept), _int32("cu_kept", cu_kept, cs.batch + 1),
+                                _int32("lengths", lengths, cs.batch), to_table.stride(0), to_table.shape[1], kept.numel(), first, 0)
+        rc = self.lib.ficoco_cache_compact(self.h, cs, a, _current_stream(cache.device) if stream is None else stream)
+        if rc:
+            _check(self.h, rc)
+        return lengths
 
     # -- status / inspection ----------------------------------------------------------------
     def ficoco_status(self, stream: Optional[int] = None) -> int:

@@ -1,0 +1,305 @@
+// Entry points of the 8-bit paged cache (ficoco.h: append, attention, weights, copy, compact) and the host's page pool.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <functional>
+#include <new>
+#include <queue>
+#include <vector>
+
+#include "../../include/ficoco.h"
+#include "cache_common.cuh"
+#include "ctx_access.h"
+#include "kernels_cache_pages.cuh"
+#include "kernels_cache_simt.cuh"
+
+using namespace ficoco;
+
+namespace {
+
+template <class... KArgs, class... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+
+int check_cache(const ficoco_cache* c, CacheView* v) {
+  if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->page_table || !c->lengths) return FICOCO_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->batch < 1 || c->max_pages < 1) return FICOCO_ERR_INVALID_ARG;
+  if (c->table_stride < c->max_pages) return FICOCO_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return FICOCO_ERR_INVALID_ARG;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return FICOCO_ERR_UNSUPPORTED;
+  if (c->head_dim % 16 != 0 || c->head_dim > 256 || c->kv_heads > 1024 || c->batch > 65535) return FICOCO_ERR_UNSUPPORTED;
+  if ((long long)c->n_pages * c->kv_heads * c->page_size > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;   // rows of a tensor map
+  if ((long long)c->max_pages * c->page_size > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
+  v->k = (uint8_t*)c->k_codes; v->v = (uint8_t*)c->v_codes; v->ks = c->k_scale; v->vs = c->v_scale;
+  v->table = c->page_table; v->len = c->lengths; v->table_stride = c->table_stride;
+  v->n_pages = c->n_pages; v->page = c->page_size; v->kv = c->kv_heads; v->dim = c->head_dim;
+  v->batch = c->batch; v->max_pages = c->max_pages;
+  v->log_page = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
+  return FICOCO_OK;
+}
+
+// Rows of a call: pointer (none where there are no rows), stride, element type.
+int check_rows(const void* p, int rows, long long stride, int dtype, long long row_elems) {
+  if (rows < 0 || (rows > 0 && !p) || !aligned16(p) || stride < row_elems) return FICOCO_ERR_INVALID_ARG;
+  if (dtype != FICOCO_FP32 && dtype != FICOCO_BF16) return FICOCO_ERR_UNSUPPORTED;
+  const int es = dtype == FICOCO_BF16 ? 2 : 4;
+  return stride * es % 16 == 0 ? FICOCO_OK : FICOCO_ERR_INVALID_ARG;
+}
+
+int check_attention(const ficoco_cache* c, const ficoco_attention_args* a) {
+  if (!a || !a->cu_rows || a->heads < 1) return FICOCO_ERR_INVALID_ARG;
+  const int rc = check_rows(a->q, a->rows, a->q_stride, a->dtype, (long long)a->heads * c->head_dim);
+  if (rc) return rc;
+  if (a->heads % c->kv_heads != 0 || a->window < 0 || a->sinks < 0) return FICOCO_ERR_INVALID_ARG;
+  if (!(a->scale > 0.f) || !isfinite(a->scale)) return FICOCO_ERR_INVALID_ARG;
+  if (a->flags & ~(unsigned)FICOCO_CAUSAL) return FICOCO_ERR_INVALID_ARG;
+  if (a->heads > 65535) return FICOCO_ERR_UNSUPPORTED;
+  return FICOCO_OK;
+}
+MaskRule mask_rule(const ficoco_attention_args* a) {
+  return MaskRule{a->window, a->window > 0 ? a->sinks : 0, (a->flags & FICOCO_CAUSAL) ? 1 : 0};
+}
+
+#define CACHE_TRY(ctx, expr)                                  \
+  do {                                                        \
+    const cudaError_t e__ = (expr);                           \
+    if (e__ != cudaSuccess) return ctx_cuda_error((ctx), e__); \
+  } while (0)
+
+}  // namespace
+
+extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_append_args* a, void* cuda_stream) {
+  if (!ctx || !a) return FICOCO_ERR_INVALID_ARG;
+  CacheView c;
+  int rc = check_cache(cache, &c);
+  if (rc) return rc;
+  if (!a->cu_rows) return FICOCO_ERR_INVALID_ARG;
+  const long long width = (long long)c.kv * c.dim;
+  if ((rc = check_rows(a->k, a->rows, a->k_stride, a->dtype, width)) || (rc = check_rows(a->v, a->rows, a->v_stride, a->dtype, width))) return rc;
+  const CtxAccess x = ctx_access(ctx);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  CACHE_TRY(ctx, cudaSetDevice(x.device));
+  ctx_set_launches(ctx, 0);
+  if (a->rows == 0) return FICOCO_OK;
+  const dim3 grid(a->rows / c.page + 2 * c.batch, c.kv);
+  ctx_prof_tick(ctx, st, "k_cache_append");
+  if (a->dtype == FICOCO_BF16)
+    CACHE_TRY(ctx, launch(k_cache_append<__nv_bfloat16>, grid, PAGE_THREADS, 0, st, c, (const __nv_bfloat16*)a->k,
+                          (const __nv_bfloat16*)a->v, a->cu_rows, a->k_stride, a->v_stride, a->rows, x.status));
+  else
+    CACHE_TRY(ctx, launch(k_cache_append<float>, grid, PAGE_THREADS, 0, st, c, (const float*)a->k, (const float*)a->v,
+                          a->cu_rows, a->k_stride, a->v_stride, a->rows, x.status));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_attention_args* a, void* cuda_stream) {
+  if (!ctx) return FICOCO_ERR_INVALID_ARG;
+  CacheView c;
+  int rc = check_cache(cache, &c);
+  if (rc || (rc = check_attention(cache, a))) return rc;
+  if ((a->rows > 0 && !a->out) || !aligned16(a->out)) return FICOCO_ERR_INVALID_ARG;
+  const size_t es = a->dtype == FICOCO_BF16 ? 2 : 4, width = (size_t)a->heads * c.dim;
+  if (a->rows > 0 && overlap(a->out, a->rows * width * es, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es))
+    return FICOCO_ERR_INVALID_ARG;
+  const CtxAccess x = ctx_access(ctx);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  CACHE_TRY(ctx, cudaSetDevice(x.device));
+  ctx_set_launches(ctx, 0);
+  if (a->rows == 0) return FICOCO_OK;
+  const float scale_log2 = a->scale * 1.4426950408889634f;
+  const dim3 grid(a->rows, a->heads);
+  ctx_prof_tick(ctx, st, "k_cache_attention_simt");
+  if (a->dtype == FICOCO_BF16)
+    CACHE_TRY(ctx, launch(k_cache_attention_simt<__nv_bfloat16>, grid, CS_THREADS, 0, st, c, (const __nv_bfloat16*)a->q,
+                          a->cu_rows, (__nv_bfloat16*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads,
+                          mask_rule(a), x.status));
+  else
+    CACHE_TRY(ctx, launch(k_cache_attention_simt<float>, grid, CS_THREADS, 0, st, c, (const float*)a->q, a->cu_rows,
+                          (float*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a), x.status));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_attention_args* a, int n_text,
+                                    int first, int count, float* weights, void* cuda_stream) {
+  if (!ctx) return FICOCO_ERR_INVALID_ARG;
+  CacheView c;
+  int rc = check_cache(cache, &c);
+  if (rc || (rc = check_attention(cache, a))) return rc;
+  if ((a->rows > 0 && !a->lse) || !weights || ((uintptr_t)weights & 3) || n_text < 1 || first < 0 || count < 1) return FICOCO_ERR_INVALID_ARG;
+  if ((long long)c.batch * n_text > INT32_MAX || (long long)first + count > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
+  const CtxAccess x = ctx_access(ctx);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  CACHE_TRY(ctx, cudaSetDevice(x.device));
+  const float scale_log2 = a->scale * 1.4426950408889634f;
+  const dim3 grid(c.batch * n_text, a->heads);
+  ctx_prof_tick(ctx, st, "k_cache_weights_simt");
+  if (a->dtype == FICOCO_BF16)
+    CACHE_TRY(ctx, launch(k_cache_weights_simt<__nv_bfloat16>, grid, CS_THREADS, 0, st, c, (const __nv_bfloat16*)a->q,
+                          a->cu_rows, a->lse, weights, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a), n_text,
+                          first, count, x.status));
+  else
+    CACHE_TRY(ctx, launch(k_cache_weights_simt<float>, grid, CS_THREADS, 0, st, c, (const float*)a->q, a->cu_rows, a->lse,
+                          weights, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a), n_text, first, count, x.status));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_cache_copy(ficoco_ctx* ctx, const ficoco_cache* cache, const int* src, const int* dst, int n, void* cuda_stream) {
+  if (!ctx) return FICOCO_ERR_INVALID_ARG;
+  CacheView c;
+  const int rc = check_cache(cache, &c);
+  if (rc) return rc;
+  if (n < 0 || (n > 0 && (!src || !dst || src == dst))) return FICOCO_ERR_INVALID_ARG;
+  const CtxAccess x = ctx_access(ctx);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  CACHE_TRY(ctx, cudaSetDevice(x.device));
+  ctx_set_launches(ctx, 0);
+  if (n == 0) return FICOCO_OK;
+  const size_t words = (size_t)c.kv * c.page * c.dim / 16;        // at most 2 M (1024 heads x 128 tokens x 256)
+  const int parts = (int)std::min<size_t>(std::max<size_t>(1, words / (4 * COPY_THREADS)), 64);
+  ctx_prof_tick(ctx, st, "k_cache_copy");
+  CACHE_TRY(ctx, launch(k_cache_copy, dim3(n, parts), COPY_THREADS, 0, st, c, src, dst, (int)words, x.status));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_compact_args* a, void* cuda_stream) {
+  if (!ctx || !a) return FICOCO_ERR_INVALID_ARG;
+  CacheView c;
+  const int rc = check_cache(cache, &c);
+  if (rc) return rc;
+  if (!a->to_table || !a->cu_kept || a->n_kept < 0 || (a->n_kept > 0 && !a->kept) || a->first < 0 || a->to_pages < 1 ||
+      a->to_stride < a->to_pages || a->to_table == c.table || a->lengths_out == c.len)
+    return FICOCO_ERR_INVALID_ARG;
+  if ((long long)a->n_kept + (long long)c.batch * a->first > INT32_MAX / 2) return FICOCO_ERR_UNSUPPORTED;
+  const CtxAccess x = ctx_access(ctx);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  CACHE_TRY(ctx, cudaSetDevice(x.device));
+  const dim3 grid((unsigned)(((long long)a->n_kept + (long long)c.batch * a->first) / c.page + 2 * c.batch), c.kv);
+  ctx_prof_tick(ctx, st, "k_cache_compact");
+  CACHE_TRY(ctx, launch(k_cache_compact, grid, PAGE_THREADS, 0, st, c, a->to_table, a->kept, a->cu_kept, a->lengths_out,
+                        a->to_stride, a->to_pages, a->n_kept, a->first, x.status));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+
+// ---- page pool (host) ---------------------------------------------------------------------------------------------
+struct ficoco_pool {
+  std::vector<int> holders;                                                     // per page; 0: free
+  std::priority_queue<int, std::vector<int>, std::greater<int>> free_pages;     // lowest first
+};
+
+extern "C" int ficoco_pool_create(ficoco_pool** out, int n_pages) {
+  if (!out || n_pages < 1) return FICOCO_ERR_INVALID_ARG;
+  try {
+    ficoco_pool* p = new ficoco_pool();
+    try {
+      p->holders.assign(n_pages, 0);
+      std::vector<int> all(n_pages);
+      for (int i = 0; i < n_pages; ++i) all[i] = i;
+      p->free_pages = decltype(p->free_pages)(std::greater<int>(), std::move(all));
+    } catch (...) {
+      delete p;
+      throw;
+    }
+    *out = p;
+    return FICOCO_OK;
+  } catch (...) {                                     // out of memory: nothing crosses the C boundary
+    return FICOCO_ERR_PAGES;
+  }
+}
+
+extern "C" int ficoco_pool_destroy(ficoco_pool* p) {
+  if (!p) return FICOCO_ERR_INVALID_ARG;
+  delete p;
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_pool_free_pages(const ficoco_pool* p) { return p ? (int)p->free_pages.size() : FICOCO_ERR_INVALID_ARG; }
+
+extern "C" int ficoco_pool_take(ficoco_pool* p, int n, int* pages) {
+  if (!p || n < 0 || (n > 0 && !pages)) return FICOCO_ERR_INVALID_ARG;
+  if ((size_t)n > p->free_pages.size()) return FICOCO_ERR_PAGES;
+  for (int i = 0; i < n; ++i) {
+    pages[i] = p->free_pages.top();
+    p->free_pages.pop();
+    p->holders[pages[i]] = 1;
+  }
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_pool_give(ficoco_pool* p, int n, const int* pages) {
+  if (!p || n < 0 || (n > 0 && !pages)) return FICOCO_ERR_INVALID_ARG;
+  // all or nothing: a list may hold a page as often as it has holders
+  int done = 0;
+  for (; done < n; ++done) {
+    const int g = pages[done];
+    if (g < 0 || g >= (int)p->holders.size() || p->holders[g] < 1) break;
+    --p->holders[g];
+  }
+  if (done < n) {
+    while (done-- > 0) ++p->holders[pages[done]];
+    return FICOCO_ERR_PAGES;
+  }
+  try {
+    for (int i = 0; i < n; ++i) {
+      const int g = pages[i];
+      if (p->holders[g] != 0) continue;
+      p->holders[g] = -1;                             // (so that a page given twice in one list is queued once)
+      p->free_pages.push(g);
+    }
+  } catch (...) {
+  }
+  for (int i = 0; i < n; ++i)
+    if (p->holders[pages[i]] < 0) p->holders[pages[i]] = 0;
+  return FICOCO_OK;
+}
+
+extern "C" int ficoco_pool_fork(ficoco_pool* p, int page_size, int length, const int* pages, int* forked, int* copy_from,
+                                int* copy_to) {
+  if (!p || page_size < 1 || length < 0 || !copy_from || !copy_to) return FICOCO_ERR_INVALID_ARG;
+  *copy_from = *copy_to = -1;
+  const int full = length / page_size, part = length % page_size ? 1 : 0;
+  if (full + part == 0) return FICOCO_OK;
+  if (!pages || !forked) return FICOCO_ERR_INVALID_ARG;
+  for (int i = 0; i < full + part; ++i)
+    if (pages[i] < 0 || pages[i] >= (int)p->holders.size() || p->holders[pages[i]] < 1) return FICOCO_ERR_PAGES;
+  if (part && p->free_pages.empty()) return FICOCO_ERR_PAGES;
+  for (int i = 0; i < full; ++i) {
+    forked[i] = pages[i];
+    ++p->holders[pages[i]];
+  }
+  if (part) {
+    const int rc = ficoco_pool_take(p, 1, copy_to);
+    if (rc) return rc;
+    *copy_from = pages[full];
+    forked[full] = *copy_to;
+  }
+  return FICOCO_OK;
+}

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/ficoco.h"
+#include "ctx_access.h"
 #include "common.cuh"
 #include "correlate_plan.h"
 #include "filter_plan.h"
@@ -209,6 +210,10 @@ struct ficoco_ctx {
   char* sch_base = nullptr;
   size_t sch_bytes = 0;
 
+  // scratch of the 8-bit cache (ctx_access.h), allocated by its first user
+  char* cache_base = nullptr;
+  size_t cache_bytes = 0;
+
   // grow-only staging for the host-buffer entry points
   char* hs_dev = nullptr;
   size_t hs_dev_bytes = 0;
@@ -288,6 +293,38 @@ extern "C" int ficoco_profile_read(ficoco_ctx* c, int index, char* name, int nam
   return FICOCO_OK;
 }
 
+namespace ficoco {
+
+CtxAccess ctx_access(const ficoco_ctx* c) { return CtxAccess{c->device, c->num_sms, c->status, c->wait_ns}; }
+int ctx_cuda_error(ficoco_ctx* c, cudaError_t e) {
+  c->last_cuda = (int)e;
+  return FICOCO_ERR_CUDA;
+}
+void ctx_set_launches(ficoco_ctx* c, int n) { c->launches = n; }
+void ctx_prof_tick(ficoco_ctx* c, cudaStream_t st, const char* name) { prof_tick(c, st, name); }
+
+int ctx_cache_scratch(ficoco_ctx* c, cudaStream_t st, size_t bytes, int** counters, float** partials) {
+  const size_t need = CACHE_COUNTERS * sizeof(int) + bytes;
+  if (need > c->cache_bytes) {
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    CUDA_TRY(c, cudaStreamIsCapturing(st, &cap));
+    if (cap != cudaStreamCaptureStatusNone) return FICOCO_ERR_CAPTURE;
+    CUDA_TRY(c, cudaDeviceSynchronize());
+    if (c->cache_base) cudaFree(c->cache_base);
+    c->cache_base = nullptr;
+    c->cache_bytes = 0;
+    CUDA_TRY(c, cudaMalloc((void**)&c->cache_base, need));
+    c->cache_bytes = need;
+    CUDA_TRY(c, cudaMemset(c->cache_base, 0, CACHE_COUNTERS * sizeof(int)));
+    CUDA_TRY(c, cudaDeviceSynchronize());
+  }
+  *counters = (int*)c->cache_base;
+  *partials = (float*)(c->cache_base + CACHE_COUNTERS * sizeof(int));
+  return FICOCO_OK;
+}
+
+}  // namespace ficoco
+
 extern "C" const char* ficoco_strerror(int code) {
   switch (code) {
     case FICOCO_OK: return "ok";
@@ -297,11 +334,12 @@ extern "C" const char* ficoco_strerror(int code) {
     case FICOCO_ERR_WORKSPACE: return "problem exceeds the sizes given to ficoco_create";
     case FICOCO_ERR_CUDA: return "CUDA runtime error";
     case FICOCO_ERR_TIMEOUT: return "device-side wait timed out";
-    case FICOCO_ERR_CAPTURE: return "a new plan cannot be uploaded during stream capture";
+    case FICOCO_ERR_CAPTURE: return "a new plan cannot be uploaded, or scratch allocated, during stream capture";
     case FICOCO_ERR_GRID: return "grid smaller than the number of alive patches";
     case FICOCO_ERR_STATIC_LIMIT:
       return "problem exceeds the fixed scratch of the allocation-free entry point "
              "(at most 64 images, dim 2048, 32768 patch tokens in total)";
+    case FICOCO_ERR_PAGES: return "not enough free pages, or a page that is not held";
     default: return "unknown error";
   }
 }
@@ -513,6 +551,7 @@ extern "C" int ficoco_destroy(ficoco_ctx* c) {
   if (c->h_stage) cudaFreeHost(c->h_stage);
   if (c->hs_dev) cudaFree(c->hs_dev);
   if (c->sch_base) cudaFree(c->sch_base);
+  if (c->cache_base) cudaFree(c->cache_base);
   if (c->hs_stream) cudaStreamDestroy(c->hs_stream);
   if (c->hs_run) cudaStreamDestroy(c->hs_run);
   if (c->hs_out) cudaStreamDestroy(c->hs_out);
@@ -1379,6 +1418,7 @@ extern "C" int ficoco_status(ficoco_ctx* c, void* cuda_stream, int* device_statu
     // a kernel gave up half-way: its per-image counters may be left non-zero
     CUDA_TRY(c, cudaMemsetAsync(c->img_cnt, 0, 6 * (size_t)c->max_batch * sizeof(int), st));
     CUDA_TRY(c, cudaMemsetAsync(c->tile_cnt, 0, (size_t)c->cap_corr * sizeof(int), st));
+    if (c->cache_base) CUDA_TRY(c, cudaMemsetAsync(c->cache_base, 0, CACHE_COUNTERS * sizeof(int), st));
     CUDA_TRY(c, cudaStreamSynchronize(st));
   }
   *device_status = (int)v;
