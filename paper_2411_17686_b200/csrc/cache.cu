@@ -14,6 +14,7 @@
 #include "ctx_access.h"
 #include "kernels_cache_pages.cuh"
 #include "kernels_cache_simt.cuh"
+#include "kernels_cache_step.cuh"
 
 using namespace ficoco;
 
@@ -85,6 +86,60 @@ MaskRule mask_rule(const ficoco_attention_args* a) {
     if (e__ != cudaSuccess) return ctx_cuda_error((ctx), e__); \
   } while (0)
 
+// Tensor maps over the code arrays: rows of head_dim bytes, boxes of a page, the swizzle of a row's width.
+typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+int code_map(ficoco_ctx* ctx, const CacheView& c, const uint8_t* codes, CUtensorMap* map) {
+  static const encode_fn encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return (encode_fn)f;
+  }();
+  if (!encode) return ctx_cuda_error(ctx, cudaErrorNotSupported);
+  const cuuint64_t dims[2] = {(cuuint64_t)c.dim, (cuuint64_t)c.n_pages * c.kv * c.page}, strides[1] = {(cuuint64_t)c.dim};
+  const cuuint32_t box[2] = {(cuuint32_t)c.dim, (cuuint32_t)c.page}, step[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? FICOCO_OK : ctx_cuda_error(ctx, cudaErrorInvalidValue);
+}
+
+// Scratch for the partial results of cut items: two per CTA, the largest of them.
+constexpr int SCRATCH_CTAS_PER_SM = 2;
+size_t scratch_bytes(const CtxAccess& x) {
+  return (size_t)x.num_sms * SCRATCH_CTAS_PER_SM * 2 * StepPlan<128, 2, 16>::PART * sizeof(float);
+}
+
+template <class T, int DIM, int NT, int RB>
+int attend_step(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
+  using PL = StepPlan<DIM, NT, RB>;
+  static_assert(PL::PART <= StepPlan<128, 2, 16>::PART, "the scratch holds it");
+  int* counters;
+  float* partials;
+  int rc = ctx_cache_scratch(ctx, st, scratch_bytes(x), &counters, &partials);
+  if (rc) return rc;
+  CUtensorMap km, vm;
+  if ((rc = code_map(ctx, c, c.k, &km)) || (rc = code_map(ctx, c, c.v, &vm))) return rc;
+  CACHE_TRY(ctx, cudaFuncSetAttribute(k_cache_step<T, DIM, NT, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM));
+  ctx_prof_tick(ctx, st, "k_cache_step");
+  CACHE_TRY(ctx, launch(k_cache_step<T, DIM, NT, RB>, dim3(x.num_sms * SCRATCH_CTAS_PER_SM), STEP_THREADS, PL::SMEM, st, km, vm, c,
+                        (const T*)a->q, a->cu_rows, (T*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a),
+                        counters, partials, x.status, x.wait_ns));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+template <int DIM>
+int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
+  if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, st);
+  const long long rows = (long long)a->rows * (a->heads / c.kv);       // of all sequences, per key/value head
+  if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, st);
+  return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, st);
+}
+
 }  // namespace
 
 extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_append_args* a, void* cuda_stream) {
@@ -128,6 +183,8 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   ctx_set_launches(ctx, 0);
   if (a->rows == 0) return FICOCO_OK;
   const float scale_log2 = a->scale * 1.4426950408889634f;
+  if (c.dim == 128) return attend_dim<128>(ctx, x, c, a, scale_log2, st);
+  if (c.dim == 64) return attend_dim<64>(ctx, x, c, a, scale_log2, st);
   const dim3 grid(a->rows, a->heads);
   ctx_prof_tick(ctx, st, "k_cache_attention_simt");
   if (a->dtype == FICOCO_BF16)
