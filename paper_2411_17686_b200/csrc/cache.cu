@@ -73,7 +73,7 @@ int check_attention(const ficoco_cache* c, const ficoco_attention_args* a) {
   if (a->heads % c->kv_heads != 0 || a->window < 0 || a->sinks < 0) return FICOCO_ERR_INVALID_ARG;
   if (!(a->scale > 0.f) || !isfinite(a->scale)) return FICOCO_ERR_INVALID_ARG;
   if (a->flags & ~(unsigned)FICOCO_CAUSAL) return FICOCO_ERR_INVALID_ARG;
-  if (a->heads > 65535) return FICOCO_ERR_UNSUPPORTED;
+  if (a->heads > 65535 || (long long)a->rows * a->heads > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
   return FICOCO_OK;
 }
 MaskRule mask_rule(const ficoco_attention_args* a) {

@@ -5,22 +5,27 @@
 // query rows are the columns.  With s_j the score in units of log2 and e_j = log2 of the page's value scale, the
 // running maximum is that of t_j = s_j + e_j, the weights are P_j = 2^(t_j - max), so that codes can be summed without their scale,
 // and the denominator sums P_j / 2^e_j.  Rows and weights are split into NT e4m3 terms (cache_umma.cuh), one more block of
-// columns each.  Every tile's O^T is added to fp32 registers.
+// columns each.
+//
+// The maximum is a warp's own: warp w works on tokens 32 w .. 32 w + 31 of every tile, which are one K step of the second
+// product, so each step gets an accumulator of its own and the four are joined, with the factors that bring them to one
+// maximum, where they are added to the fp32 sums in registers.  No barrier stands between a tile's scores and its weights.
 //
 // What bounds it: HBM, one byte per key or value element.  The tensor cores are idle most of the time and nothing is
-// converted, so an SM needs 200 to 300 instructions per warp and tile of 32 KB.  All tiles of all (sequence, row block, head)
+// converted, so an SM needs about 200 instructions per warp and tile of 32 KB.  All tiles of all (sequence, row block, head)
 // items form one list which is cut into equal pieces, one per CTA (two CTAs per SM, so that one's softmax runs under the other's
 // loads): ragged lengths balance by themselves.  An item that is cut leaves partial results; the CTA that finishes
 // it last joins them in the order of the list, so the result does not depend on who that was.
 //
-// Roles: warps 0-3 softmax and epilogue (thread = token, then dimension), warp 4 TMA and page scales, warp 5 MMA.  Tile i's
-// scores are computed while tile i - 1's weights are multiplied.
+// Roles: warps 0-3 softmax (thread = token of the tile), warps 4-7 queries and output (thread = dimension), warp 8 TMA and
+// page scales, warp 9 MMA.  Tile i's scores are computed while tile i - 1's weights are multiplied; keys are given back as
+// soon as the scores exist; queries are two items ahead, page indexes two and scales one batch of 32 / (pages per tile) tiles.
 #pragma once
 #include "cache_umma.cuh"
 
 namespace ficoco {
 
-constexpr int STEP_THREADS = 192;
+constexpr int STEP_THREADS = 320;
 constexpr int STEP_MAX_PARTS = 64;         // most pieces that an item is cut into
 
 // One sequence of the call, in tiles.
@@ -30,11 +35,11 @@ struct StepSeq {
 __device__ __forceinline__ StepSeq step_seq(const CacheView& c, const int* cu, int rows, int group, int rb, const MaskRule& mask,
                                             int b, unsigned* status) {
   StepSeq s;
+  s.len = cache_length(c, b, status);
   const int2 r = cache_rows(cu, b, rows, status);
   s.row0 = r.x;
   s.n_rows = r.y - r.x;
-  s.len = s.n_rows > 0 ? cache_length(c, b, status) : 0;
-  s.blocks = (int)(((long long)s.n_rows * group + rb - 1) / rb);
+  s.blocks = (int)(((uint32_t)s.n_rows * (uint32_t)group + rb - 1) / rb);
   // tokens that some row sees: the first sinks and everything from the first row's window on
   const int lo = mask.window > 0 ? min(max(0, s.len - s.n_rows - mask.window + 1), s.len) : 0;
   s.t0 = lo / CTILE;
@@ -49,30 +54,30 @@ struct StepSeg {
   StepSeq s;
 };
 struct StepWalk {
-  long long at, end;                       // in the list
-  long long first;                         // where sequence b starts in it
-  int b;
+  long long left;                          // tiles of the piece that are still to come
+  int b, head, block, tile;
   StepSeq s;
 };
 __device__ __forceinline__ bool step_next(StepWalk& w, StepSeg& g, const CacheView& c, const int* cu, int rows, int group, int rb,
                                           const MaskRule& mask, unsigned* status) {
-  if (w.at >= w.end) return false;
-  for (;;) {
-    const long long size = (long long)w.s.blocks * c.kv * w.s.nt;
-    if (w.at < w.first + size || w.b + 1 >= c.batch) break;
-    w.first += size;
+  if (w.left <= 0) return false;
+  if (w.tile >= w.s.nt) {
+    w.tile = 0;
+    if (++w.head == c.kv) { w.head = 0; ++w.block; }
+  }
+  while (w.block >= w.s.blocks && w.b + 1 < c.batch) {
+    w.block = 0;
     w.s = step_seq(c, cu, rows, group, rb, mask, ++w.b, status);
   }
-  const long long off = w.at - w.first;
-  const int item = (int)(off / w.s.nt);
-  g.b = w.b;
-  g.s = w.s;
-  g.head = item % c.kv;
-  g.block = item / c.kv;
-  g.tile = (int)(off - (long long)item * w.s.nt);
-  g.count = (int)min((long long)(w.s.nt - g.tile), w.end - w.at);
-  w.at += g.count;
+  g.b = w.b; g.head = w.head; g.block = w.block; g.tile = w.tile; g.s = w.s;
+  g.count = (int)min((long long)(w.s.nt - w.tile), w.left);
+  w.tile += g.count;
+  w.left -= g.count;
   return true;
+}
+// x * y / z for y, z < 512; in 32 bits where the product fits (a 64-bit division is some 100 instructions)
+__device__ __forceinline__ long long mul_div(long long x, int y, int z) {
+  return x < (1 << 23) ? (long long)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
 }
 __device__ __forceinline__ int step_token0(const StepSeq& s, int tile) {      // first token of a tile of the item
   return (tile < s.t_sink ? tile : tile - s.t_sink + s.t0) * CTILE;
@@ -81,16 +86,55 @@ __device__ __forceinline__ int step_token0(const StepSeq& s, int tile) {      //
 template <int DIM, int NT, int RB>
 struct StepPlan {
   static constexpr int N = NT * RB;                                  // columns of both products
-  static constexpr int STAGE = 2 * CTILE * DIM;                      // keys and values of a tile
+  static constexpr int HALF = CTILE * DIM;                           // keys or values of a tile
   static constexpr int Q_BYTES = (N * DIM + 1023) / 1024 * 1024, P_BYTES = N * CTILE;
-  static constexpr int ROOM = 112 * 1024 - 2048;                     // half an SM's shared memory, less what is static
-  static constexpr int STAGES_FIT = (ROOM - 1024 - 2 * (Q_BYTES + P_BYTES)) / STAGE;
+  static constexpr int ROOM = 112 * 1024 - 3072;                     // half an SM's shared memory, less what is static
+  static constexpr int STAGES_FIT = (ROOM - 1024 - 2 * (Q_BYTES + P_BYTES)) / (2 * HALF);
   static constexpr int STAGES = STAGES_FIT > 6 ? 6 : STAGES_FIT;
-  static constexpr int SMEM = 1024 + STAGES * STAGE + 2 * (Q_BYTES + P_BYTES);
-  static constexpr int TMEM = 4 * N <= 64 ? 64 : 4 * N <= 128 ? 128 : 256;
+  static constexpr int SMEM = 1024 + STAGES * 2 * HALF + 2 * (Q_BYTES + P_BYTES);
+  // 256 of the SM's 512 TMEM columns: score buffers of N and output buffers of 4 N columns
+  static constexpr int NS = 10 * N <= 256 || 6 * N <= 256 ? 2 : 1, NO = 10 * N <= 256 ? 2 : 1;
+  static constexpr int TMEM = 256;
   static constexpr int PART = RB * (DIM + 2);                        // floats of a partial result
-  static_assert(STAGES >= 2 && 4 * N <= 256 && N % 16 == 0, "two CTAs per SM");
+  static_assert(STAGES >= 2 && (NS + 4 * NO) * N <= TMEM && N % 16 == 0, "two CTAs per SM");
 };
+
+// Sums of x[0 .. RB) over the warp; lane r (r < RB) gets that of x[r].  Halves the values that a lane holds with every
+// exchange: RB - 1 shuffles and as many more as are left of the five steps, not five for each value.
+template <int RB>
+__device__ __forceinline__ float warp_sums(float (&x)[RB], int lane) {
+#pragma unroll
+  for (int bit = RB / 2; bit > 0; bit >>= 1) {
+    const bool up = lane & bit;
+#pragma unroll
+    for (int r = 0; r < bit; ++r) {
+      const float keep = up ? x[r + bit] : x[r], give = up ? x[r] : x[r + bit];
+      x[r] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, bit);
+    }
+  }
+  float v = x[0];
+#pragma unroll
+  for (int bit = RB; bit < 32; bit <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, bit);
+  return v;
+}
+
+// This thread's lane of the RB sums whose terms are NT blocks of RB accumulator columns, smallest term first.
+template <int NT, int RB>
+__device__ __forceinline__ void load_sums(uint32_t taddr, float (&x)[RB]) {
+  static_assert(RB == 8 || RB == 16, "16 columns are two terms or one");
+#pragma unroll
+  for (int n = NT * RB - 16; n >= 0; n -= 16) {
+    float f[16];
+    ctmem_ld16(taddr + n, f);
+    ctmem_wait_ld();
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      if (n + 16 == NT * RB) x[r] = f[16 - RB + r];
+      else x[r] = fmaf(x[r], 0.0625f, f[16 - RB + r]);
+      if (RB == 8) x[r] = fmaf(x[r], 0.0625f, f[r]);
+    }
+  }
+}
 
 template <class T, int DIM, int NT, int RB>
 __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
@@ -99,48 +143,61 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     float scale_log2, int rows, int heads, const MaskRule mask, int* __restrict__ counters, float* __restrict__ partials,
     unsigned* __restrict__ status, unsigned long long wait_ns) {
   using PL = StepPlan<DIM, NT, RB>;
-  constexpr int N = PL::N, NST = PL::STAGES;
+  constexpr int N = PL::N, NST = PL::STAGES, NS = PL::NS, NO = PL::NO;
   extern __shared__ unsigned char step_raw[];
-  __shared__ uint64_t full_bar[NST], empty_bar[NST], q_bar[2], s_bar[2], p_bar[2], o_bar[2], drain_bar;
+  __shared__ uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST], scale_bar[NST];
+  __shared__ uint64_t q_bar[2], s_bar[2], s_free[2], p_bar[2], o_bar[2], free_bar[2], l_bar[2], drain_bar;
   __shared__ uint32_t tmem_s;
   __shared__ float page_scale[NST][3][8];              // key scale, log2 of the value scale, 1 / value scale
-  __shared__ __align__(16) float wmax[2][4][RB];
-  __shared__ float lred[4][RB];
+  __shared__ float wmax[2][4][RB];                     // running maxima of the softmax warps, behind a tile
+  __shared__ __align__(16) float factor[2][4][5][RB];  // per output warp: what brings the four warps' sums, and the old ones, to one maximum
+  __shared__ float l_s[2][4][RB];                      // denominators of an item, per softmax warp
   __shared__ float q_scale[2][RB];
   __shared__ int2 row_see[2][RB];                      // tokens [x, y) of a row (and its sinks)
-  __shared__ long long scan[STEP_THREADS / 32][2], start_s[4];
-  __shared__ int scan_b, failed, last_s;
+  __shared__ long long scan[STEP_THREADS / 32][2];
+  __shared__ StepWalk start_s;
+  __shared__ StepSeg seg_s[4];                         // the output warps' items: this one and the two ahead
+  __shared__ int failed, last_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t ring = (smem_u32(step_raw) + 1023u) & ~1023u;
-  const uint32_t q_base = ring + NST * PL::STAGE, p_base = q_base + 2 * PL::Q_BYTES;
+  const uint32_t ring = (smem_u32(step_raw) + 1023u) & ~1023u;         // keys of all stages, then values
+  const uint32_t v_ring = ring + NST * PL::HALF, q_base = v_ring + NST * PL::HALF, p_base = q_base + 2 * PL::Q_BYTES;
   const int group = heads / c.kv;
   if (tid == 0) {
-    for (int s = 0; s < NST; ++s) { mbar_init(&full_bar[s], 2); mbar_init(&empty_bar[s], 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&q_bar[s], 128); mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 128); mbar_init(&o_bar[s], 1); }
+    for (int s = 0; s < NST; ++s) {
+      mbar_init(&k_full[s], 1); mbar_init(&v_full[s], 1); mbar_init(&k_empty[s], 1); mbar_init(&v_empty[s], 1);
+      mbar_init(&scale_bar[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&q_bar[s], 128); mbar_init(&s_bar[s], 1); mbar_init(&s_free[s], 4); mbar_init(&p_bar[s], 4);
+      mbar_init(&o_bar[s], 1); mbar_init(&free_bar[s], 4); mbar_init(&l_bar[s], 4);
+    }
     mbar_init(&drain_bar, 1);
-    scan_b = -1;
+    start_s.left = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 5) tmem_alloc(&tmem_s, PL::TMEM);
+  if (warp == 9) tmem_alloc(&tmem_s, PL::TMEM);
   grid_dep_wait();
   if (tid == 0) failed = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
 
   // ---- this CTA's piece of the list: a thread sums the tiles of a run of sequences -----------------------------------------
   const int per = (c.batch + STEP_THREADS - 1) / STEP_THREADS, b_lo = min(tid * per, c.batch), b_hi = min(b_lo + per, c.batch);
-  long long mine = 0, most = 0;
+  long long mine = 0;
+  int most = 0;
+  StepSeq s0;
+  s0.nt = 1;
   for (int b = b_lo; b < b_hi; ++b) {
-    const StepSeq s = step_seq(c, cu, rows, group, RB, mask, b, status);
-    mine += (long long)s.blocks * c.kv * s.nt;
-    most = max(most, (long long)(s.blocks > 0 ? s.nt : 0));
+    s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
+    mine += (long long)s0.blocks * c.kv * s0.nt;
+    if (s0.blocks > 0) most = max(most, s0.nt);
   }
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
     if (lane >= o) upto += v;
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
   }
+  most = __reduce_max_sync(0xFFFFFFFFu, most);
   if (lane == 31) { scan[warp][0] = upto; scan[warp][1] = most; }
   ctc_fence_before();
   __syncthreads();
@@ -155,78 +212,135 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     nt_most = max(nt_most, scan[w][1]);
   }
   // CTAs that get a piece: no more than tiles, nor so many that the longest item would be cut into more than STEP_MAX_PARTS
-  long long n_cta = min((long long)gridDim.x, total);
-  if (nt_most > 0) n_cta = max(1ll, min(n_cta, (STEP_MAX_PARTS - 1) * total / nt_most));
-  StepWalk walk;
-  walk.at = blockIdx.x < n_cta ? total * blockIdx.x / n_cta : 0;
-  walk.end = blockIdx.x < n_cta ? total * (blockIdx.x + 1) / n_cta : 0;
-  if (walk.at < walk.end && walk.at >= upto - mine && walk.at < upto) {      // one thread's run holds the start
+  int n_cta = (int)min((long long)gridDim.x, total);
+  if ((long long)n_cta * nt_most > (STEP_MAX_PARTS - 1) * total) n_cta = (int)max(1ll, (STEP_MAX_PARTS - 1) * total / nt_most);
+  const bool has_piece = (int)blockIdx.x < n_cta && failed == 0;
+  const long long piece0 = has_piece ? mul_div(total, blockIdx.x, n_cta) : 0;
+  const long long piece1 = has_piece ? mul_div(total, blockIdx.x + 1, n_cta) : 0;
+  if (piece0 < piece1 && piece0 >= upto - mine && piece0 < upto) {           // one thread's run holds the start
     long long at = upto - mine;
     int b = b_lo;
-    for (; b + 1 < b_hi; ++b) {
-      const StepSeq s = step_seq(c, cu, rows, group, RB, mask, b, status);
-      const long long size = (long long)s.blocks * c.kv * s.nt;
-      if (walk.at < at + size) break;
+    for (; b + 1 < b_hi; ++b) {                                              // (a run of one sequence is at hand)
+      s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
+      const long long size = (long long)s0.blocks * c.kv * s0.nt;
+      if (piece0 < at + size) break;
       at += size;
     }
-    start_s[0] = at;
-    scan_b = b;
+    if (per > 1 && b + 1 == b_hi) s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
+    const long long off = piece0 - at;
+    const long long item = off < (1ll << 32) ? (long long)((uint32_t)off / (uint32_t)s0.nt) : off / s0.nt;
+    start_s.s = s0;
+    start_s.b = b;
+    start_s.tile = (int)(off - item * s0.nt);
+    start_s.block = (int)(item / c.kv);
+    start_s.head = (int)(item - (long long)start_s.block * c.kv);
+    start_s.left = piece1 - piece0;
   }
   __syncthreads();
-  const bool idle = walk.at >= walk.end || failed != 0 || scan_b < 0;
-  if (!idle) {
-    walk.b = scan_b;
-    walk.first = start_s[0];
-    walk.s = step_seq(c, cu, rows, group, RB, mask, walk.b, status);
-  } else {
-    walk.at = walk.end = 0;
-  }
-  bool ok = true;
+  StepWalk walk = start_s;
+  bool ok = true;                                      // the same in all lanes of a warp
+  auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
 
-  if (warp == 4) {
-    // ---------------- TMA: lane p brings page p of a tile ----------------------------------------------------------------
+  if (warp == 8) {
+    // ---------------- TMA.  Lane = (tile of a batch, page of the tile) -------------------------------------------------------
+    const int log_ppt = 7 - c.log_page, ppt = 1 << log_ppt, batch_tiles = 32 >> log_ppt, my_page = lane & (ppt - 1);
     StepSeg g;
-    int i = 0, st = 0;
-    uint32_t par = 1;
-    while (ok && step_next(walk, g, c, cu, rows, group, RB, mask, status)) {
-      for (int t = g.tile; t < g.tile + g.count; ++t, ++i) {
-        const int base = step_token0(g.s, t), left = min(CTILE, g.s.len - base);
-        const int pages = left > 0 ? (left + c.page - 1) >> c.log_page : 0;
-        int page = 0;
-        if (lane < pages) page = cache_page(c, g.b, (base >> c.log_page) + lane, 0, status);
-        if (i >= NST) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty_bar[st], par, wait_ns));
-        if (!ok) break;
-        const uint32_t bytes = (uint32_t)(c.page * DIM);
-        if (lane == 0) mbar_expect_tx(&full_bar[st], 2u * bytes * (uint32_t)pages);
-        __syncwarp();
-        const size_t at = (size_t)page * c.kv + g.head;
-        if (lane < pages) {
-          const uint32_t dst = ring + (uint32_t)st * PL::STAGE + (uint32_t)lane * bytes;
-          tma_rows(dst, &kmap, (int)(at << c.log_page), &full_bar[st]);
-          tma_rows(dst + CTILE * DIM, &vmap, (int)(at << c.log_page), &full_bar[st]);
-          const float sv = c.vs[at];
-          page_scale[st][0][lane] = c.ks[at];
-          page_scale[st][1][lane] = log2f(sv);
-          page_scale[st][2][lane] = 1.0f / sv;
+    int t_next = 0, t_end = 0;
+    struct Batch { int page, head, tiles; float ks, vs; };
+    // The next batch: this lane's page (-1: none) and head, tiles in the batch.
+    auto assign = [&](Batch& x) {
+      x.tiles = 0;
+      x.page = -1;
+      x.ks = x.vs = 1.f;
+      int b = 0, entry = -1;
+      for (; x.tiles < batch_tiles; ++x.tiles, ++t_next) {
+        if (t_next >= t_end) {
+          if (!step_next(walk, g, c, cu, rows, group, RB, mask, status)) break;
+          t_next = g.tile;
+          t_end = g.tile + g.count;
         }
+        if (lane >> log_ppt == x.tiles) {
+          const int base = step_token0(g.s, t_next);
+          b = g.b;
+          x.head = g.head;
+          entry = base + (my_page << c.log_page) < g.s.len ? (base >> c.log_page) + my_page : -1;
+        }
+      }
+      if (entry >= 0) x.page = cache_page(c, b, entry, 0, status);
+    };
+    auto fetch_scales = [&](Batch& x) {
+      if (x.page >= 0) {
+        const size_t at = (size_t)x.page * c.kv + x.head;
+        x.ks = c.ks[at];
+        x.vs = c.vs[at];
+      }
+    };
+    Batch now, soon, later;
+    now.head = soon.head = later.head = 0;
+    assign(now);
+    fetch_scales(now);
+    const uint32_t bytes = (uint32_t)(c.page * DIM);
+    int i = 0, st = 0, wrap = -1, st_before = 0;
+    float v3[3];                                         // scales of the tile before this one, whose turn is one tile late:
+    bool held = false;                                   // the first batch's are still on their way when its copies go out
+    auto deliver = [&]() {
+      if (held) {
+#pragma unroll
+        for (int x = 0; x < 3; ++x) page_scale[st_before][x][my_page] = v3[x];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&scale_bar[st_before]);
+    };
+    bool first = true;
+    while (ok && now.tiles > 0) {
+      if (!first) { fetch_scales(soon); assign(later); }
+      for (int t = 0; t < now.tiles; ++t, ++i) {
+        const bool mine_now = lane >> log_ppt == t && now.page >= 0;
+        const uint32_t load = bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine_now));
+        const uint32_t dst = ring + (uint32_t)st * PL::HALF + (uint32_t)my_page * bytes;
+        const int row = (now.page * c.kv + now.head) << c.log_page;
+        if (i >= NST) wait(&k_empty[st], wrap);
+        if (ok) {
+          if (lane == 0) mbar_expect_tx(&k_full[st], load);
+          __syncwarp();
+          if (mine_now) tma_rows(dst, &kmap, row, &k_full[st]);
+          if (i >= NST) wait(&v_empty[st], wrap);
+          if (!ok && lane == 0) mbar_wait(&k_full[st], (uint32_t)(wrap + 1) & 1u, wait_ns);
+        }
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(&v_full[st], load);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full_bar[st]);
-        if (++st == NST) { st = 0; par ^= 1u; }
+        if (mine_now) tma_rows(dst + NST * PL::HALF, &vmap, row, &v_full[st]);
+        if (i > 0) deliver();
+        held = mine_now;
+        if (mine_now) { v3[0] = now.ks; v3[1] = log2f(now.vs); v3[2] = 1.0f / now.vs; }
+        st_before = st;
+        if (++st == NST) { st = 0; ++wrap; }
+        if (first && (t + 1 == now.tiles || t + 1 == NST)) {     // the ring is full: time for the batches behind
+          first = false;
+          assign(soon);
+          fetch_scales(soon);
+          assign(later);
+        }
+      }
+      now = soon;
+      soon = later;
+    }
+    if (i > 0 && ok) deliver();
+    if (!ok) {
+      if (lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+      // no copy outlives the CTA: the tiles asked for last
+      for (int k = max(0, i - NST); k < i; ++k) {
+        mbar_wait(&k_full[k % NST], (k / NST) & 1, wait_ns);
+        mbar_wait(&v_full[k % NST], (k / NST) & 1, wait_ns);
       }
     }
-    if (!ok) {
-      atomicOr(status, STATUS_TIMEOUT);
-      // no copy outlives the CTA: the tiles asked for last
-      for (int k = max(0, i - NST); k < i; ++k) mbar_wait(&full_bar[k % NST], (k / NST) & 1, wait_ns);
-      failed = 1;
-    }
-  } else if (warp == 5) {
-    // ---------------- MMA: scores of tile i + 1 go out before the weights of tile i are waited for ------------------------
+  } else if (warp == 9) {
+    // ---------------- MMA: scores of tile i go out before the weights of tile i - 1 are waited for ------------------------
     const uint32_t u_tmem = __shfl_sync(0xFFFFFFFFu, tmem, 0);
     constexpr uint32_t id_s = cache_idesc(128, N, 0, 0), id_o = cache_idesc(DIM, N, 1, 0);
     StepSeg g;
-    int seg = -1, left = 0, st = 0, st_prev = 0;
-    uint32_t par = 0;
+    int seg = -1, left = 0, st = 0, wrap = 0, st_prev = 0, wrap_prev = 0;
     for (int i = 0;; ++i) {
       bool more = true;
       if (left == 0) {
@@ -234,56 +348,147 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         if (more) {
           ++seg;
           left = g.count;
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait(&q_bar[seg & 1], (seg >> 1) & 1, wait_ns));
-          if (!ok) break;
+          wait(&q_bar[seg & 1], seg >> 1);
         }
       }
       if (more) {
         --left;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full_bar[st], par, wait_ns));
+        wait(&k_full[st], wrap);
+        if (i >= NS) wait(&s_free[i % NS], (i / NS) - 1);
         if (!ok) break;
         ctc_fence_after();
-        const uint32_t a = ring + (uint32_t)st * PL::STAGE, b = q_base + (uint32_t)(seg & 1) * PL::Q_BYTES;
-        const uint64_t ad = cache_desc<DIM>(a), bd = cache_desc<DIM>(b);
+        const uint64_t ad = cache_desc<DIM>(ring + (uint32_t)st * PL::HALF);
+        const uint64_t bd = cache_desc<DIM>(q_base + (uint32_t)(seg & 1) * PL::Q_BYTES);
 #pragma unroll
-        for (int k = 0; k < DIM / 32; ++k) mma_f8(u_tmem + (uint32_t)(i & 1) * N, ad + 2 * k, bd + 2 * k, id_s, k > 0);
-        mma_commit(&s_bar[i & 1]);
+        for (int k = 0; k < DIM / 32; ++k) mma_f8(u_tmem + (uint32_t)(i % NS) * N, ad + 2 * k, bd + 2 * k, id_s, k > 0);
+        mma_commit(&s_bar[i % NS]);
+        mma_commit(&k_empty[st]);
       }
       if (i > 0) {
         const int j = i - 1;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&p_bar[j & 1], (j >> 1) & 1, wait_ns));
+        wait(&v_full[st_prev], wrap_prev);
+        wait(&p_bar[j & 1], j >> 1);
+        if (NO == 1 && j > 0) wait(&free_bar[(j - 1) & 1], (j - 1) >> 1);
         if (!ok) break;
         ctc_fence_after();
-        const uint64_t ad = cache_desc<DIM>(ring + (uint32_t)st_prev * PL::STAGE + CTILE * DIM);
+        const uint64_t ad = cache_desc<DIM>(v_ring + (uint32_t)st_prev * PL::HALF);
         const uint64_t bd = cache_desc<128>(p_base + (uint32_t)(j & 1) * PL::P_BYTES);
 #pragma unroll
-        for (int k = 0; k < CTILE / 32; ++k)
-          mma_f8(u_tmem + 2 * N + (uint32_t)(j & 1) * N, ad + (uint64_t)(k * (32 * DIM >> 4)), bd + 2 * k, id_o, k > 0);
-        mma_commit(&o_bar[j & 1]);
-        mma_commit(&empty_bar[st_prev]);
+        for (int k = 0; k < 4; ++k)      // a softmax warp's tokens each, into columns of its own
+          mma_f8(u_tmem + NS * N + (uint32_t)((j % NO) * 4 + k) * N, ad + (uint64_t)(k * (32 * DIM >> 4)), bd + 2 * k, id_o, 0);
+        mma_commit(&o_bar[j % NO]);
+        mma_commit(&v_empty[st_prev]);
       }
       if (!more) break;
       st_prev = st;
-      if (++st == NST) { st = 0; par ^= 1u; }
+      wrap_prev = wrap;
+      if (++st == NST) { st = 0; ++wrap; }
     }
     if (!ok) {
-      atomicOr(status, STATUS_TIMEOUT);
+      if (lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
       mma_commit(&drain_bar);
       mbar_wait(&drain_bar, 0, wait_ns);
-      failed = 1;
     }
-  } else {
-    // ---------------- softmax: thread = token of the tile, then dimension of the output ------------------------------------
+  } else if (warp < 4) {
+    // ---------------- softmax: thread = token of the tile; the warps go their own ways ------------------------------------
     const uint32_t t_lane = tmem + ((uint32_t)(warp * 32) << 16);
+    StepSeg g;
+    int i = 0, st = 0, wrap = 0;
+    const int pg = tid >> c.log_page;
+    for (int seg = 0; ok && step_next(walk, g, c, cu, rows, group, RB, mask, status); ++seg) {
+      const int buf_q = seg & 1;
+      wait(&q_bar[buf_q], seg >> 1);                           // the rows' scales and masks
+      float m[RB], l[RB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) { m[r] = -CUDART_INF_F; l[r] = 0.f; }
+      // a tile inside [in_lo, in_hi) is seen by every row of the item
+      const int i_first = (int)((uint32_t)g.block * RB / (uint32_t)group);
+      const int i_last = min((int)(((uint32_t)g.block * RB + RB - 1) / (uint32_t)group), g.s.n_rows - 1);
+      const int in_hi = seen(mask, g.s.len - g.s.n_rows + i_first, g.s.len).z;
+      const int in_lo = seen(mask, g.s.len - g.s.n_rows + i_last, g.s.len).y;
+      for (int t = g.tile; t < g.tile + g.count; ++t, ++i) {
+        const int base = step_token0(g.s, t), buf = i & 1;
+        wait(&scale_bar[st], wrap);
+        const bool token = base + tid < g.s.len;               // (pages behind the last one have no scales)
+        const float ks = page_scale[st][0][pg], ve = page_scale[st][1][pg], vi = token ? page_scale[st][2][pg] : 0.f;
+        wait(&s_bar[i % NS], i / NS);
+        if (!ok) break;
+        ctc_fence_after();
+        float s[RB];
+        load_sums<NT, RB>(t_lane + (uint32_t)(i % NS) * N, s);
+        ctc_fence_before();
+        if (lane == 0) mbar_arrive(&s_free[i % NS]);
+        const bool edge = base < in_lo || base + CTILE > in_hi;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) s[r] = fmaf(s[r], q_scale[buf_q][r] * ks, ve);
+        if (edge) {
+          const int j = base + tid;
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            const int2 see = row_see[buf_q][r];
+            const bool on = j < see.y && (j >= see.x || j < mask.sinks);
+            s[r] = on ? s[r] : -CUDART_INF_F;
+          }
+          if (base + CTILE > g.s.len) {                        // no token: whatever the slot holds must not meet a weight of 0
+            wait(&v_full[st], wrap);
+            if (!ok) break;
+            if (!token) {
+              const uint32_t v = v_ring + (uint32_t)st * PL::HALF + tid * DIM;
+#pragma unroll
+              for (int x = 0; x < DIM; x += 16) st_shared16(v + x, 0u, 0u, 0u, 0u);
+            }
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          const float mn = fmaxf(m[r], warp_max(s[r])), ref = mn == -CUDART_INF_F ? 0.f : mn;
+          const float corr = ex2(m[r] - ref);
+          m[r] = mn;
+          s[r] = ex2(s[r] - ref);
+          l[r] = fmaf(l[r], corr, s[r] * vi);
+        }
+        if (i >= 2) wait(&free_bar[buf], (i >> 1) - 1);        // the weights and maxima of tile i - 2 have been used
+        if (!ok) break;
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+          if (lane == r) wmax[buf][warp][r] = m[r];
+        const uint32_t p = p_base + (uint32_t)buf * PL::P_BYTES + (tid & 15);
+#pragma unroll
+        for (int r = 0; r < RB; r += 2) {
+          uint32_t code[NT];
+          split_pair<NT>(s[r] * 256.f, s[r + 1] * 256.f, code);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) {
+            const int n = u * RB + r;
+            st_shared1(p + n * 128 + ((((tid >> 4) ^ n) & 7) << 4), code[u] & 0xFFu);
+            st_shared1(p + (n + 1) * 128 + ((((tid >> 4) ^ (n + 1)) & 7) << 4), code[u] >> 8);
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_bar[buf]);
+        if (++st == NST) { st = 0; ++wrap; }
+      }
+      if (!ok) break;
+      const float sum = warp_sums<RB>(l, lane);
+      if (lane < RB) l_s[buf_q][warp][lane] = sum;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&l_bar[buf_q]);
+    }
+    if (!ok && lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+  } else {
+    // ---------------- queries and output: thread = dimension -------------------------------------------------------------
+    const int bt = tid - 128, bw = warp - 4;
+    const uint32_t t_lane = tmem + ((uint32_t)(bw * 32) << 16);
     constexpr int LANES = DIM / 8, PASS_ROWS = 128 / LANES, PASSES = (RB + PASS_ROWS - 1) / PASS_ROWS;
-    const int q_chunk = tid % LANES, q_row = tid / LANES;
+    const int q_chunk = bt % LANES, q_row = bt / LANES;
     float qf[PASSES][8];
     // rows of an item: row x of block k is head x % group of the sequence's row x / group
     auto load_q = [&](const StepSeg& g) {
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
-        const long long x = (long long)g.block * RB + p * PASS_ROWS + q_row;
-        const int i = (int)(x / group), h = g.head * group + (int)(x - (long long)i * group);
+        const uint32_t x = (uint32_t)g.block * RB + p * PASS_ROWS + q_row;
+        const int i = (int)(x / (uint32_t)group), h = g.head * group + (int)(x - (uint32_t)i * group);
         const bool on = p * PASS_ROWS + q_row < RB && i < g.s.n_rows;
         if (on) load8(q + (long long)(g.s.row0 + i) * q_stride + (long long)h * DIM + q_chunk * 8, qf[p]);
         else {
@@ -300,179 +505,141 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         const float s = store_query<DIM, NT>(qf[p], q_base + (uint32_t)buf * PL::Q_BYTES, r, RB, q_chunk);
         if (q_chunk == 0) q_scale[buf][r] = s * scale_log2;
       }
-      if (tid < RB) {
-        const long long x = (long long)g.block * RB + tid;
-        const int i = (int)min(x / group, (long long)g.s.n_rows);
+      if (bt < RB) {
+        const uint32_t x = (uint32_t)g.block * RB + bt;
+        const int i = min((int)(x / (uint32_t)group), g.s.n_rows);
         const int3 see = seen(mask, g.s.len - g.s.n_rows + i, g.s.len);
-        row_see[buf][tid] = i < g.s.n_rows ? make_int2(see.y, see.z) : make_int2(0, 0);
+        row_see[buf][bt] = i < g.s.n_rows ? make_int2(see.y, see.z) : make_int2(0, 0);
       }
       fence_proxy_async();
       mbar_arrive(&q_bar[buf]);
     };
-    StepSeg g, g_next;
-    bool have = step_next(walk, g, c, cu, rows, group, RB, mask, status);
-    long long seg_at = walk.at;                                // end of segment g in the list
-    if (have) { load_q(g); put_q(g, 0); }
-    cta_sync(1, 128);                                          // the rows' scales and masks are in shared memory
-    int i = 0, st = 0, seg = 0;
-    uint32_t par = 0;
-    float m[RB], l[RB], acc[RB];
-    while (have) {
-      seg_at = walk.at;
-      const bool have_next = step_next(walk, g_next, c, cu, rows, group, RB, mask, status);
-      if (have_next) load_q(g_next);
+    // item k's description goes to seg_s[k % 4]; returns whether there is one, its query rows asked for
+    auto ahead = [&](int k) {
+      StepSeg g;
+      if (!step_next(walk, g, c, cu, rows, group, RB, mask, status)) return false;
+      load_q(g);
+      if (bt == 0) seg_s[k & 3] = g;
+      return true;
+    };
+    long long at = piece0;                                     // where this item's tiles start in the list
+    int n_seg = 0;                                             // items described so far
+    for (; n_seg < 3 && ahead(n_seg); ++n_seg) {
+      cta_sync(2, 128);
+      if (n_seg < 2) put_q(seg_s[n_seg], n_seg);
+    }
+    bool more = n_seg == 3;
+    int i = 0;
+    constexpr int PER = RB / 8;                                // maxima per lane: lane = (softmax warp, row % 8)
+    for (int seg = 0; seg < n_seg; ++seg) {
       const int buf_q = seg & 1;
+      const StepSeg& g = seg_s[seg & 3];
+      const int count = g.count;
+      float acc[RB], m_run[PER];
 #pragma unroll
-      for (int r = 0; r < RB; ++r) { m[r] = -CUDART_INF_F; l[r] = 0.f; acc[r] = 0.f; }
-      // a tile inside [in_lo, in_hi) is seen by every row of the item
-      const int i_first = (int)((long long)g.block * RB / group);
-      const int i_last = (int)min(((long long)g.block * RB + RB - 1) / group, (long long)g.s.n_rows - 1);
-      const int in_hi = seen(mask, g.s.len - g.s.n_rows + i_first, g.s.len).z;
-      const int in_lo = seen(mask, g.s.len - g.s.n_rows + i_last, g.s.len).y;
-      for (int t = g.tile; t < g.tile + g.count; ++t, ++i) {
-        const int base = step_token0(g.s, t), buf = i & 1;
-        if (ok) ok = mbar_wait(&full_bar[st], par, wait_ns);   // (page scales; and values, where they are cleared below)
-        const int pg = tid >> c.log_page;
-        const bool token = base + tid < g.s.len;               // (pages behind the last one have no scales)
-        const float ks = page_scale[st][0][pg], ve = page_scale[st][1][pg], vi = token ? page_scale[st][2][pg] : 0.f;
-        if (ok) ok = mbar_wait(&s_bar[buf], (i >> 1) & 1, wait_ns);
+      for (int r = 0; r < RB; ++r) acc[r] = 0.f;
+#pragma unroll
+      for (int p = 0; p < PER; ++p) m_run[p] = -CUDART_INF_F;
+      for (int t = 1; t <= count; ++t, ++i) {
+        const int buf = i & 1;
+        wait(&p_bar[buf], i >> 1);                             // the maxima
+        float (*f)[RB] = factor[buf][bw];
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+          const int w = lane >> 3, r = (lane & 7) + 8 * p;
+          const float mw = wmax[buf][w][r];
+          float mn = fmaxf(m_run[p], mw);
+          mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 8));
+          mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 16));
+          const float ref = mn == -CUDART_INF_F ? 0.f : mn;
+          f[w][r] = ex2(mw - ref);
+          if (w == 0) f[4][r] = ex2(m_run[p] - ref);
+          m_run[p] = mn;
+        }
+        __syncwarp();
+        wait(&o_bar[i % NO], i / NO);
         ctc_fence_after();
-        float s[N];
 #pragma unroll
-        for (int n = 0; n < N; n += 16) ctmem_ld16(t_lane + (uint32_t)buf * N + n, s + n);
-        ctmem_wait_ld();
-        const bool edge = base < in_lo || base + CTILE > in_hi;
-        const int j = base + tid;
+        for (int r = 0; r < RB; ++r) acc[r] *= f[4][r];
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          float x = s[(NT - 1) * RB + r];
+        for (int w = 0; w < 4; ++w) {
+          float o[RB];
+          load_sums<NT, RB>(t_lane + NS * N + (uint32_t)((i % NO) * 4 + w) * N, o);
 #pragma unroll
-          for (int u = NT - 2; u >= 0; --u) x = fmaf(x, 0.0625f, s[u * RB + r]);
-          s[r] = fmaf(x, q_scale[buf_q][r] * ks, ve);
+          for (int r = 0; r < RB; ++r) acc[r] = fmaf(o[r], f[w][r], acc[r]);
         }
-        if (edge) {
-#pragma unroll
-          for (int r = 0; r < RB; ++r) {
-            const int2 see = row_see[buf_q][r];
-            const bool on = j < see.y && (j >= see.x || j < mask.sinks);
-            s[r] = on ? s[r] : -CUDART_INF_F;
-          }
-          if (!token) {                                        // no token: whatever the slot holds must not meet a weight of 0
-            const uint32_t v = ring + (uint32_t)st * PL::STAGE + CTILE * DIM + tid * DIM;
-#pragma unroll
-            for (int x = 0; x < DIM; x += 16) st_shared16(v + x, 0u, 0u, 0u, 0u);
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const float x = warp_max(s[r]);
-          if (lane == r) wmax[buf][warp][r] = x;
-        }
-        // a wait that ran out anywhere ends the loop for all 128 threads
-        if (cta_sync_or(1, 128, !ok)) { ok = false; break; }
-        float corr[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const float x = fmaxf(fmaxf(wmax[buf][0][r], wmax[buf][1][r]), fmaxf(wmax[buf][2][r], wmax[buf][3][r]));
-          const float mn = fmaxf(m[r], x), ref = mn == -CUDART_INF_F ? 0.f : mn;
-          corr[r] = ex2(m[r] - ref);
-          m[r] = mn;
-          s[r] = ex2(s[r] - ref);
-          l[r] = fmaf(l[r], corr[r], s[r] * vi);
-        }
-        const uint32_t p = p_base + (uint32_t)buf * PL::P_BYTES;
-#pragma unroll
-        for (int r = 0; r < RB; r += 2) {
-          uint32_t code[NT];
-          split_pair<NT>(s[r] * 256.f, s[r + 1] * 256.f, code);
-#pragma unroll
-          for (int u = 0; u < NT; ++u) {
-            const int n = u * RB + r;
-            st_shared1(p + n * 128 + ((((tid >> 4) ^ n) & 7) << 4) + (tid & 15), code[u] & 0xFFu);
-            st_shared1(p + (n + 1) * 128 + ((((tid >> 4) ^ (n + 1)) & 7) << 4) + (tid & 15), code[u] >> 8);
-          }
-        }
-        fence_proxy_async();
         ctc_fence_before();
-        mbar_arrive(&p_bar[buf]);
-        if (t == g.tile) {
-          if (have_next) put_q(g_next, buf_q ^ 1);
-        } else {                                               // what the tile before this one added
-          if (ok) ok = mbar_wait(&o_bar[buf ^ 1], ((i - 1) >> 1) & 1, wait_ns);
-          ctc_fence_after();
-          float o[N];
-#pragma unroll
-          for (int n = 0; n < N; n += 16) ctmem_ld16(t_lane + 2 * N + (uint32_t)(buf ^ 1) * N + n, o + n);
-          ctmem_wait_ld();
-#pragma unroll
-          for (int r = 0; r < RB; ++r) {
-            float x = o[(NT - 1) * RB + r];
-#pragma unroll
-            for (int u = NT - 2; u >= 0; --u) x = fmaf(x, 0.0625f, o[u * RB + r]);
-            acc[r] = (acc[r] + x) * corr[r];
-          }
-          ctc_fence_before();
-        }
-        if (++st == NST) { st = 0; par ^= 1u; }
+        __syncwarp();
+        if (t < count && lane == 0) mbar_arrive(&free_bar[buf]);
       }
-      if (!ok) break;
-      if (ok) ok = mbar_wait(&o_bar[(i - 1) & 1], ((i - 1) >> 1) & 1, wait_ns);
-      ctc_fence_after();
+      wait(&l_bar[buf_q], seg >> 1);
+      float l[RB];
       {
-        float o[N];
-#pragma unroll
-        for (int n = 0; n < N; n += 16) ctmem_ld16(t_lane + 2 * N + (uint32_t)((i - 1) & 1) * N + n, o + n);
-        ctmem_wait_ld();
+        const float (*f)[RB] = factor[(i - 1) & 1][bw];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-          float x = o[(NT - 1) * RB + r];
+          l[r] = 0.f;
 #pragma unroll
-          for (int u = NT - 2; u >= 0; --u) x = fmaf(x, 0.0625f, o[u * RB + r]);
-          acc[r] += x;
+          for (int w = 0; w < 4; ++w) l[r] = fmaf(l_s[buf_q][w][r], f[w][r], l[r]);
         }
-        ctc_fence_before();
       }
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const float x = warp_sum(l[r]);
-        if (lane == 0) lred[warp][r] = x;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&free_bar[(i - 1) & 1]);
+      if (cta_sync_or(2, 128, !ok)) { ok = false; break; }     // one wait that ran out ends it for all 128 threads
+      if (seg + 2 < n_seg) put_q(seg_s[(seg + 2) & 3], buf_q); // (every score of this item is computed and used)
+      if (more) {
+        more = ahead(n_seg);
+        n_seg += more;
       }
-      if (cta_sync_or(1, 128, !ok)) { ok = false; break; }
-#pragma unroll
-      for (int r = 0; r < RB; ++r) l[r] = (lred[0][r] + lred[1][r]) + (lred[2][r] + lred[3][r]);
       // (M = 64 accumulators lie in the first sixteen lanes of each warp)
       const bool has_dim = DIM == 128 || lane < 16;
-      const int d = DIM == 128 ? tid : warp * 16 + lane;
-      const int x0 = g.block * RB, nr = (int)min((long long)RB, (long long)g.s.n_rows * group - x0);
-      if (g.count == g.s.nt) {
+      const int d = DIM == 128 ? bt : bw * 16 + lane;
+      const int x0 = g.block * RB, nr = min(RB, g.s.n_rows * group - x0);
+      if (count == g.s.nt) {
+        const int ri = x0 / group, h0 = x0 - ri * group;
+        long long o_at = (long long)(g.s.row0 + ri) * heads + g.head * group + h0;
+        int h = h0;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
           if (r < nr) {
-            const int ri = (x0 + r) / group, h = g.head * group + (x0 + r) - ri * group;
-            const long long at = (long long)(g.s.row0 + ri) * heads + h;
-            if (has_dim) store1(out + at * DIM + d, l[r] > 0.f || l[r] != l[r] ? acc[r] * (0.00390625f / l[r]) : 0.f);
-            if (lse != nullptr && tid == r) lse[at] = l[r] > 0.f || l[r] != l[r] ? (m[r] + log2f(l[r])) * 0.69314718055994531f : -CUDART_INF_F;
+            const bool some = l[r] > 0.f || l[r] != l[r];
+            if (has_dim) store1(out + o_at * DIM + d, some ? acc[r] * __fdividef(0.00390625f, l[r]) : 0.f);
+            if (lse != nullptr) {
+              const float top = __shfl_sync(0xFFFFFFFFu, m_run[r / 8], r & 7);
+              if (bt == r) lse[o_at] = some ? (top + log2f(l[r])) * 0.69314718055994531f : -CUDART_INF_F;
+            }
+            ++o_at;
+            if (++h == group) { h = 0; o_at += heads - group; }
           }
         }
       } else {
         // A cut item.  Its first piece is the last one of CTA `owner`, the others are the first ones of the CTAs behind it.
-        const long long item0 = seg_at - g.count - g.tile, item1 = item0 + g.s.nt;
-        auto cta_of = [&](long long x) { return (int)(((x + 1) * n_cta + total - 1) / total - 1); };
+        const long long item0 = at - g.tile, item1 = item0 + g.s.nt;
+        auto cta_of = [&](long long x) {
+          int k = (int)((float)(x + 1) * (float)n_cta / (float)total);
+          k = min(max(k, 0), n_cta - 1);
+          while (mul_div(total, k, n_cta) > x) --k;
+          while (mul_div(total, k + 1, n_cta) <= x) ++k;
+          return k;
+        };
         const int owner = cta_of(item0), parts = cta_of(item1 - 1) - owner + 1;
         float* mine_p = partials + ((size_t)blockIdx.x * 2 + (g.tile == 0 ? 1 : 0)) * PL::PART;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-          if (has_dim) __stcg(mine_p + r * DIM + d, acc[r]);
-          if (tid == r) { __stcg(mine_p + RB * DIM + r, m[r]); __stcg(mine_p + RB * DIM + RB + r, l[r]); }
+          if (r < nr) {
+            if (has_dim) __stcg(mine_p + r * DIM + d, acc[r]);
+            const float top = __shfl_sync(0xFFFFFFFFu, m_run[r / 8], r & 7);
+            if (bt == r) { __stcg(mine_p + RB * DIM + r, top); __stcg(mine_p + RB * DIM + RB + r, l[r]); }
+          }
         }
-        cta_sync(1, 128);
-        if (tid == 0) last_s = atom_acq_rel_add(&counters[owner], 1) == parts - 1;
-        cta_sync(1, 128);
+        cta_sync(2, 128);
+        if (bt == 0) last_s = atom_acq_rel_add(&counters[owner], 1) == parts - 1;
+        cta_sync(2, 128);
         if (last_s) {
-          if (tid == 0) counters[owner] = 0;
+          if (bt == 0) counters[owner] = 0;
           __threadfence();
           auto part = [&](int k) { return partials + ((size_t)(owner + k) * 2 + (k == 0 ? 1 : 0)) * PL::PART; };
-          for (int u = tid; u < nr * (DIM / 4); u += 128) {
+          for (int u = bt; u < nr * (DIM / 4); u += 128) {
             const int r = u / (DIM / 4), d4 = (u % (DIM / 4)) * 4;
             float top = -CUDART_INF_F;
 #pragma unroll 8
@@ -480,7 +647,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
             const float ref = top == -CUDART_INF_F ? 0.f : top;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
             float ls = 0.f;
-#pragma unroll 8
+#pragma unroll 4
             for (int k = 0; k < parts; ++k) {
               const float* pk = part(k);
               const float w = ex2(__ldcg(pk + RB * DIM + r) - ref);
@@ -490,26 +657,22 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
             }
             const bool some = ls > 0.f || ls != ls;
             const float inv = some ? 0.00390625f / ls : 0.f;
-            const int ri = (x0 + r) / group, h = g.head * group + (x0 + r) - ri * group;
-            const long long at = (long long)(g.s.row0 + ri) * heads + h;
-            T* o = out + at * DIM + d4;
+            const int rr = (x0 + r) / group, hh = g.head * group + (x0 + r) - rr * group;
+            const long long o_at = (long long)(g.s.row0 + rr) * heads + hh;
+            T* o = out + o_at * DIM + d4;
             store1(o, some ? a.x * inv : 0.f); store1(o + 1, some ? a.y * inv : 0.f);
             store1(o + 2, some ? a.z * inv : 0.f); store1(o + 3, some ? a.w * inv : 0.f);
-            if (lse != nullptr && d4 == 0) lse[at] = some ? (top + log2f(ls)) * 0.69314718055994531f : -CUDART_INF_F;
+            if (lse != nullptr && d4 == 0) lse[o_at] = some ? (top + log2f(ls)) * 0.69314718055994531f : -CUDART_INF_F;
           }
         }
       }
-      g = g_next;
-      have = have_next;
-      ++seg;
+      at += count;
     }
-    if (!ok) {
-      if (tid == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
-    }
+    if (!ok && lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
   }
   ctc_fence_before();
   __syncthreads();
-  if (warp == 5) tmem_free(tmem, PL::TMEM);
+  if (warp == 9) tmem_free(tmem, PL::TMEM);
 }
 
 }  // namespace ficoco
