@@ -88,7 +88,7 @@ struct StepPlan {
   static constexpr int N = NT * RB;                                  // columns of both products
   static constexpr int HALF = CTILE * DIM;                           // keys or values of a tile
   static constexpr int Q_BYTES = (N * DIM + 1023) / 1024 * 1024, P_BYTES = N * CTILE;
-  static constexpr int ROOM = 112 * 1024 - 3072;                     // half an SM's shared memory, less what is static
+  static constexpr int ROOM = 112 * 1024 - 3072 - RB * DIM * 4;      // half an SM's shared memory, less what is static
   static constexpr int STAGES_FIT = (ROOM - 1024 - 2 * (Q_BYTES + P_BYTES)) / (2 * HALF);
   static constexpr int STAGES = STAGES_FIT > 6 ? 6 : STAGES_FIT;
   static constexpr int SMEM = 1024 + STAGES * 2 * HALF + 2 * (Q_BYTES + P_BYTES);
@@ -98,6 +98,15 @@ struct StepPlan {
   static constexpr int PART = RB * (DIM + 2);                        // floats of a partial result
   static_assert(STAGES >= 2 && (NS + 4 * NO) * N <= TMEM && N % 16 == 0, "two CTAs per SM");
 };
+
+// x[k] without a branch (any value for k >= RB).
+template <int RB>
+__device__ __forceinline__ float pick(const float (&x)[RB], int k) {
+  float v = x[0];
+#pragma unroll
+  for (int r = 1; r < RB; ++r) v = k == r ? x[r] : v;
+  return v;
+}
 
 // Sums of x[0 .. RB) over the warp; lane r (r < RB) gets that of x[r].  Halves the values that a lane holds with every
 // exchange: RB - 1 shuffles and as many more as are left of the five steps, not five for each value.
@@ -154,10 +163,10 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
   __shared__ float l_s[2][4][RB];                      // denominators of an item, per softmax warp
   __shared__ float q_scale[2][RB];
   __shared__ int2 row_see[2][RB];                      // tokens [x, y) of a row (and its sinks)
-  __shared__ long long scan[STEP_THREADS / 32][2];
-  __shared__ StepWalk start_s;
   __shared__ StepSeg seg_s[4];                         // the output warps' items: this one and the two ahead
-  __shared__ int failed, last_s;
+  __shared__ __align__(16) float out_s[RB][DIM];       // an item's sums
+  __shared__ float top_s[RB], den_s[RB];               // its maxima and denominators
+  __shared__ int last_s, dead_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = (smem_u32(step_raw) + 1023u) & ~1023u;         // keys of all stages, then values
@@ -173,71 +182,82 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       mbar_init(&o_bar[s], 1); mbar_init(&free_bar[s], 4); mbar_init(&l_bar[s], 4);
     }
     mbar_init(&drain_bar, 1);
-    start_s.left = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) tmem_alloc(&tmem_s, PL::TMEM);
   grid_dep_wait();
-  if (tid == 0) failed = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
-
-  // ---- this CTA's piece of the list: a thread sums the tiles of a run of sequences -----------------------------------------
-  const int per = (c.batch + STEP_THREADS - 1) / STEP_THREADS, b_lo = min(tid * per, c.batch), b_hi = min(b_lo + per, c.batch);
-  long long mine = 0;
-  int most = 0;
-  StepSeq s0;
-  s0.nt = 1;
-  for (int b = b_lo; b < b_hi; ++b) {
-    s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
-    mine += (long long)s0.blocks * c.kv * s0.nt;
-    if (s0.blocks > 0) most = max(most, s0.nt);
+  // (one thread's look for the CTA: another CTA may raise the bit at any time)
+  if (tid == 0) dead_s = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
+  // ---- this CTA's piece of the list.  Every warp finds it by itself (lane = sequence), so that no barrier is waited for ------
+  StepWalk walk;
+  long long piece0, piece1, total = 0;
+  int n_cta;
+  {
+    int nt_most = 0;
+    StepSeq s0;
+    long long size = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += 32) {
+      size = 0;
+      if (b0 + lane < c.batch) {
+        s0 = step_seq(c, cu, rows, group, RB, mask, b0 + lane, status);
+        size = (long long)s0.blocks * c.kv * s0.nt;
+        if (size > 0) nt_most = max(nt_most, s0.nt);
+      }
+      total += size;
+    }
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    nt_most = __reduce_max_sync(0xFFFFFFFFu, nt_most);
+    // CTAs that get a piece: no more than tiles, nor so many that the longest item would be cut into more than STEP_MAX_PARTS
+    n_cta = (int)min((long long)gridDim.x, total);
+    if ((long long)n_cta * nt_most > (STEP_MAX_PARTS - 1) * total) n_cta = (int)max(1ll, (STEP_MAX_PARTS - 1) * total / nt_most);
+    const bool has_piece = (int)blockIdx.x < n_cta;
+    piece0 = has_piece ? mul_div(total, blockIdx.x, n_cta) : 0;
+    piece1 = has_piece ? mul_div(total, blockIdx.x + 1, n_cta) : 0;
+    walk.left = piece1 - piece0;
+    walk.b = 0; walk.head = walk.block = walk.tile = 0;
+    if (walk.left > 0) {
+      long long before = 0;
+      for (int b0 = 0;; b0 += 32) {
+        if (c.batch > 32) {                                    // (the last 32 sequences' sizes are at hand)
+          size = 0;
+          if (b0 + lane < c.batch) {
+            s0 = step_seq(c, cu, rows, group, RB, mask, b0 + lane, status);
+            size = (long long)s0.blocks * c.kv * s0.nt;
+          }
+        }
+        long long upto = size;
+#pragma unroll 1
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+          upto += lane >= o ? v : 0;
+        }
+        const unsigned reached = __ballot_sync(0xFFFFFFFFu, before + upto > piece0);
+        if (reached == 0 && b0 + 32 < c.batch) {
+          before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+          continue;
+        }
+        const int l = reached ? __ffs(reached) - 1 : 31;
+        walk.b = b0 + l;
+        walk.s.len = __shfl_sync(0xFFFFFFFFu, s0.len, l); walk.s.row0 = __shfl_sync(0xFFFFFFFFu, s0.row0, l);
+        walk.s.n_rows = __shfl_sync(0xFFFFFFFFu, s0.n_rows, l); walk.s.blocks = __shfl_sync(0xFFFFFFFFu, s0.blocks, l);
+        walk.s.t_sink = __shfl_sync(0xFFFFFFFFu, s0.t_sink, l); walk.s.t0 = __shfl_sync(0xFFFFFFFFu, s0.t0, l);
+        walk.s.nt = __shfl_sync(0xFFFFFFFFu, s0.nt, l);
+        const long long off = piece0 - before - __shfl_sync(0xFFFFFFFFu, upto - size, l);
+        const int item = (int)(off < (1ll << 32) ? (long long)((uint32_t)off / (uint32_t)walk.s.nt) : off / walk.s.nt);
+        walk.tile = (int)(off - (long long)item * walk.s.nt);
+        walk.block = (int)((uint32_t)item / (uint32_t)c.kv);
+        walk.head = item - walk.block * c.kv;
+        break;
+      }
+    }
   }
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  most = __reduce_max_sync(0xFFFFFFFFu, most);
-  if (lane == 31) { scan[warp][0] = upto; scan[warp][1] = most; }
   ctc_fence_before();
-  __syncthreads();
+  __syncthreads();                                             // barriers, TMEM
   ctc_fence_after();
   grid_dep_launch();       // behind the barrier: a dependent that took this CTA's TMEM first would wait for it for ever
   const uint32_t tmem = tmem_s;
-  long long total = 0, nt_most = 0;
-#pragma unroll
-  for (int w = 0; w < STEP_THREADS / 32; ++w) {
-    if (w < warp) upto += scan[w][0];
-    total += scan[w][0];
-    nt_most = max(nt_most, scan[w][1]);
-  }
-  // CTAs that get a piece: no more than tiles, nor so many that the longest item would be cut into more than STEP_MAX_PARTS
-  int n_cta = (int)min((long long)gridDim.x, total);
-  if ((long long)n_cta * nt_most > (STEP_MAX_PARTS - 1) * total) n_cta = (int)max(1ll, (STEP_MAX_PARTS - 1) * total / nt_most);
-  const bool has_piece = (int)blockIdx.x < n_cta && failed == 0;
-  const long long piece0 = has_piece ? mul_div(total, blockIdx.x, n_cta) : 0;
-  const long long piece1 = has_piece ? mul_div(total, blockIdx.x + 1, n_cta) : 0;
-  if (piece0 < piece1 && piece0 >= upto - mine && piece0 < upto) {           // one thread's run holds the start
-    long long at = upto - mine;
-    int b = b_lo;
-    for (; b + 1 < b_hi; ++b) {                                              // (a run of one sequence is at hand)
-      s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
-      const long long size = (long long)s0.blocks * c.kv * s0.nt;
-      if (piece0 < at + size) break;
-      at += size;
-    }
-    if (per > 1 && b + 1 == b_hi) s0 = step_seq(c, cu, rows, group, RB, mask, b, status);
-    const long long off = piece0 - at;
-    const long long item = off < (1ll << 32) ? (long long)((uint32_t)off / (uint32_t)s0.nt) : off / s0.nt;
-    start_s.s = s0;
-    start_s.b = b;
-    start_s.tile = (int)(off - item * s0.nt);
-    start_s.block = (int)(item / c.kv);
-    start_s.head = (int)(item - (long long)start_s.block * c.kv);
-    start_s.left = piece1 - piece0;
-  }
-  __syncthreads();
-  StepWalk walk = start_s;
+  if (dead_s) walk.left = 0;
   bool ok = true;                                      // the same in all lanes of a warp
   auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
 
@@ -248,25 +268,24 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     int t_next = 0, t_end = 0;
     struct Batch { int page, head, tiles; float ks, vs; };
     // The next batch: this lane's page (-1: none) and head, tiles in the batch.
-    auto assign = [&](Batch& x) {
-      x.tiles = 0;
+    auto assign = [&](Batch& x, int most) {
       x.page = -1;
       x.ks = x.vs = 1.f;
-      int b = 0, entry = -1;
-      for (; x.tiles < batch_tiles; ++x.tiles, ++t_next) {
+      int b = 0, base = 0, len = 0;
+      for (x.tiles = 0; x.tiles < most; ++x.tiles, ++t_next) {
         if (t_next >= t_end) {
           if (!step_next(walk, g, c, cu, rows, group, RB, mask, status)) break;
           t_next = g.tile;
           t_end = g.tile + g.count;
         }
-        if (lane >> log_ppt == x.tiles) {
-          const int base = step_token0(g.s, t_next);
-          b = g.b;
-          x.head = g.head;
-          entry = base + (my_page << c.log_page) < g.s.len ? (base >> c.log_page) + my_page : -1;
-        }
+        const bool on = lane >> log_ppt == x.tiles;            // (a branch that some lanes take costs 160 cycles)
+        b = on ? g.b : b;
+        base = on ? step_token0(g.s, t_next) : base;
+        len = on ? g.s.len : len;
+        x.head = on ? g.head : x.head;
       }
-      if (entry >= 0) x.page = cache_page(c, b, entry, 0, status);
+      base += my_page << c.log_page;
+      if (base < len) x.page = cache_page(c, b, base >> c.log_page, 0, status);
     };
     auto fetch_scales = [&](Batch& x) {
       if (x.page >= 0) {
@@ -277,7 +296,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     };
     Batch now, soon, later;
     now.head = soon.head = later.head = 0;
-    assign(now);
+    assign(now, min(batch_tiles, NST));
     fetch_scales(now);
     const uint32_t bytes = (uint32_t)(c.page * DIM);
     int i = 0, st = 0, wrap = -1, st_before = 0;
@@ -293,7 +312,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     };
     bool first = true;
     while (ok && now.tiles > 0) {
-      if (!first) { fetch_scales(soon); assign(later); }
+      if (!first) { fetch_scales(soon); assign(later, batch_tiles); }
       for (int t = 0; t < now.tiles; ++t, ++i) {
         const bool mine_now = lane >> log_ppt == t && now.page >= 0;
         const uint32_t load = bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine_now));
@@ -316,11 +335,11 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         if (mine_now) { v3[0] = now.ks; v3[1] = log2f(now.vs); v3[2] = 1.0f / now.vs; }
         st_before = st;
         if (++st == NST) { st = 0; ++wrap; }
-        if (first && (t + 1 == now.tiles || t + 1 == NST)) {     // the ring is full: time for the batches behind
+        if (first && t + 1 == now.tiles) {                     // the ring is full: time for the batches behind
           first = false;
-          assign(soon);
+          assign(soon, batch_tiles);
           fetch_scales(soon);
-          assign(later);
+          assign(later, batch_tiles);
         }
       }
       now = soon;
@@ -328,7 +347,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     }
     if (i > 0 && ok) deliver();
     if (!ok) {
-      if (lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+      if (lane == 0) atomicOr(status, STATUS_TIMEOUT);
       // no copy outlives the CTA: the tiles asked for last
       for (int k = max(0, i - NST); k < i; ++k) {
         mbar_wait(&k_full[k % NST], (k / NST) & 1, wait_ns);
@@ -385,7 +404,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       if (++st == NST) { st = 0; ++wrap; }
     }
     if (!ok) {
-      if (lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+      if (lane == 0) atomicOr(status, STATUS_TIMEOUT);
       mma_commit(&drain_bar);
       mbar_wait(&drain_bar, 0, wait_ns);
     }
@@ -449,9 +468,10 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         }
         if (i >= 2) wait(&free_bar[buf], (i >> 1) - 1);        // the weights and maxima of tile i - 2 have been used
         if (!ok) break;
-#pragma unroll
-        for (int r = 0; r < RB; ++r)
-          if (lane == r) wmax[buf][warp][r] = m[r];
+        {                                                      // (a store per row under `lane == r` took 160 cycles each)
+          const float mine_m = pick<RB>(m, lane);
+          if (lane < RB) wmax[buf][warp][lane] = mine_m;
+        }
         const uint32_t p = p_base + (uint32_t)buf * PL::P_BYTES + (tid & 15);
 #pragma unroll
         for (int r = 0; r < RB; r += 2) {
@@ -475,7 +495,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       __syncwarp();
       if (lane == 0) mbar_arrive(&l_bar[buf_q]);
     }
-    if (!ok && lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+    if (!ok && lane == 0) atomicOr(status, STATUS_TIMEOUT);
   } else {
     // ---------------- queries and output: thread = dimension -------------------------------------------------------------
     const int bt = tid - 128, bw = warp - 4;
@@ -573,15 +593,18 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         if (t < count && lane == 0) mbar_arrive(&free_bar[buf]);
       }
       wait(&l_bar[buf_q], seg >> 1);
-      float l[RB];
-      {
-        const float (*f)[RB] = factor[(i - 1) & 1][bw];
+      cta_sync(2, 128);                                        // the item before this one has been read
+      // (M = 64 accumulators lie in the first sixteen lanes of each warp)
+      if (DIM == 128 || lane < 16) {
+        const int d = DIM == 128 ? bt : bw * 16 + lane;
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          l[r] = 0.f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) l[r] = fmaf(l_s[buf_q][w][r], f[w][r], l[r]);
-        }
+        for (int r = 0; r < RB; ++r) out_s[r][d] = acc[r];
+      }
+      if (bw == 0 && lane < RB) {
+        const float (*f)[RB] = factor[(i - 1) & 1][0];
+        den_s[lane] = fmaf(l_s[buf_q][0][lane], f[0][lane], l_s[buf_q][1][lane] * f[1][lane]) +
+                      fmaf(l_s[buf_q][2][lane], f[2][lane], l_s[buf_q][3][lane] * f[3][lane]);
+        top_s[lane] = lane < 8 ? m_run[0] : m_run[PER - 1];
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&free_bar[(i - 1) & 1]);
@@ -591,30 +614,35 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         more = ahead(n_seg);
         n_seg += more;
       }
-      // (M = 64 accumulators lie in the first sixteen lanes of each warp)
-      const bool has_dim = DIM == 128 || lane < 16;
-      const int d = DIM == 128 ? bt : bw * 16 + lane;
-      const int x0 = g.block * RB, nr = min(RB, g.s.n_rows * group - x0);
+      // Four dimensions of a row per thread and turn (rolled loops: an item's end runs few times, and code that is fetched for the
+      // first time takes longer than what it does).
+      const uint32_t x0 = (uint32_t)g.block * RB;
+      const int nr = min(RB, (int)((uint32_t)g.s.n_rows * group - x0));
+      auto place = [&](int r) {                                // where row r of the item lies in out and lse
+        const uint32_t ri = (x0 + r) / (uint32_t)group;
+        return (long long)(g.s.row0 + (int)ri) * heads + g.head * group + (int)(x0 + r - ri * group);
+      };
+      auto finish = [&](int r, int d4, const float4& v, float top, float den) {
+        const bool some = den > 0.f || den != den;
+        const float inv = some ? __fdividef(0.00390625f, den) : 0.f;
+        const long long o_at = place(r);
+        store4(out + o_at * DIM + d4, make_float4(some ? v.x * inv : 0.f, some ? v.y * inv : 0.f, some ? v.z * inv : 0.f, some ? v.w * inv : 0.f));
+        if (lse != nullptr && d4 == 0) lse[o_at] = some ? (top + log2f(den)) * 0.69314718055994531f : -CUDART_INF_F;
+      };
       if (count == g.s.nt) {
-        const int ri = x0 / group, h0 = x0 - ri * group;
-        long long o_at = (long long)(g.s.row0 + ri) * heads + g.head * group + h0;
-        int h = h0;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          if (r < nr) {
-            const bool some = l[r] > 0.f || l[r] != l[r];
-            if (has_dim) store1(out + o_at * DIM + d, some ? acc[r] * __fdividef(0.00390625f, l[r]) : 0.f);
-            if (lse != nullptr) {
-              const float top = __shfl_sync(0xFFFFFFFFu, m_run[r / 8], r & 7);
-              if (bt == r) lse[o_at] = some ? (top + log2f(l[r])) * 0.69314718055994531f : -CUDART_INF_F;
-            }
-            ++o_at;
-            if (++h == group) { h = 0; o_at += heads - group; }
-          }
+#pragma unroll 1
+        for (int u = bt; u < nr * (DIM / 4); u += 128) {
+          const int r = u / (DIM / 4), d4 = (u % (DIM / 4)) * 4;
+          finish(r, d4, *reinterpret_cast<const float4*>(&out_s[r][d4]), top_s[r], den_s[r]);
         }
       } else {
         // A cut item.  Its first piece is the last one of CTA `owner`, the others are the first ones of the CTAs behind it.
         const long long item0 = at - g.tile, item1 = item0 + g.s.nt;
+        float* mine_p = partials + ((size_t)blockIdx.x * 2 + (g.tile == 0 ? 1 : 0)) * PL::PART;
+#pragma unroll 1
+        for (int u = bt; u < nr * (DIM / 4); u += 128)
+          __stcg(reinterpret_cast<float4*>(mine_p + u * 4), *reinterpret_cast<const float4*>(&out_s[0][0] + u * 4));
+        if (bt < nr) { __stcg(mine_p + RB * DIM + bt, top_s[bt]); __stcg(mine_p + RB * DIM + RB + bt, den_s[bt]); }
         auto cta_of = [&](long long x) {
           int k = (int)((float)(x + 1) * (float)n_cta / (float)total);
           k = min(max(k, 0), n_cta - 1);
@@ -623,52 +651,48 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
           return k;
         };
         const int owner = cta_of(item0), parts = cta_of(item1 - 1) - owner + 1;
-        float* mine_p = partials + ((size_t)blockIdx.x * 2 + (g.tile == 0 ? 1 : 0)) * PL::PART;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          if (r < nr) {
-            if (has_dim) __stcg(mine_p + r * DIM + d, acc[r]);
-            const float top = __shfl_sync(0xFFFFFFFFu, m_run[r / 8], r & 7);
-            if (bt == r) { __stcg(mine_p + RB * DIM + r, top); __stcg(mine_p + RB * DIM + RB + r, l[r]); }
-          }
-        }
         cta_sync(2, 128);
         if (bt == 0) last_s = atom_acq_rel_add(&counters[owner], 1) == parts - 1;
         cta_sync(2, 128);
         if (last_s) {
           if (bt == 0) counters[owner] = 0;
-          __threadfence();
           auto part = [&](int k) { return partials + ((size_t)(owner + k) * 2 + (k == 0 ? 1 : 0)) * PL::PART; };
+#pragma unroll 1
           for (int u = bt; u < nr * (DIM / 4); u += 128) {
             const int r = u / (DIM / 4), d4 = (u % (DIM / 4)) * 4;
-            float top = -CUDART_INF_F;
-#pragma unroll 8
-            for (int k = 0; k < parts; ++k) top = fmaxf(top, __ldcg(part(k) + RB * DIM + r));
-            const float ref = top == -CUDART_INF_F ? 0.f : top;
+            float top = -CUDART_INF_F, den = 0.f;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-            float ls = 0.f;
-#pragma unroll 4
-            for (int k = 0; k < parts; ++k) {
-              const float* pk = part(k);
-              const float w = ex2(__ldcg(pk + RB * DIM + r) - ref);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(pk + r * DIM + d4));
-              ls = fmaf(w, __ldcg(pk + RB * DIM + RB + r), ls);
-              a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
+            // four parts at a time, in order, the sums brought to the larger maximum
+#pragma unroll 1
+            for (int k0 = 0; k0 < parts; k0 += 4) {
+              float m4[4], l4[4];
+              float4 v4[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float* pk = part(min(k0 + k, parts - 1));
+                m4[k] = k0 + k < parts ? __ldcg(pk + RB * DIM + r) : -CUDART_INF_F;
+                l4[k] = __ldcg(pk + RB * DIM + RB + r);
+                v4[k] = __ldcg(reinterpret_cast<const float4*>(pk + r * DIM + d4));
+              }
+              const float mn = fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), top), ref = mn == -CUDART_INF_F ? 0.f : mn;
+              const float w0 = ex2(top - ref);
+              top = mn;
+              den *= w0; a.x *= w0; a.y *= w0; a.z *= w0; a.w *= w0;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if (k0 + k >= parts) break;
+                const float w = ex2(m4[k] - ref);
+                den = fmaf(w, l4[k], den);
+                a.x = fmaf(w, v4[k].x, a.x); a.y = fmaf(w, v4[k].y, a.y); a.z = fmaf(w, v4[k].z, a.z); a.w = fmaf(w, v4[k].w, a.w);
+              }
             }
-            const bool some = ls > 0.f || ls != ls;
-            const float inv = some ? 0.00390625f / ls : 0.f;
-            const int rr = (x0 + r) / group, hh = g.head * group + (x0 + r) - rr * group;
-            const long long o_at = (long long)(g.s.row0 + rr) * heads + hh;
-            T* o = out + o_at * DIM + d4;
-            store1(o, some ? a.x * inv : 0.f); store1(o + 1, some ? a.y * inv : 0.f);
-            store1(o + 2, some ? a.z * inv : 0.f); store1(o + 3, some ? a.w * inv : 0.f);
-            if (lse != nullptr && d4 == 0) lse[o_at] = some ? (top + log2f(ls)) * 0.69314718055994531f : -CUDART_INF_F;
+            finish(r, d4, a, top, den);
           }
         }
       }
       at += count;
     }
-    if (!ok && lane == 0) { atomicOr(status, STATUS_TIMEOUT); failed = 1; }
+    if (!ok && lane == 0) atomicOr(status, STATUS_TIMEOUT);
   }
   ctc_fence_before();
   __syncthreads();
