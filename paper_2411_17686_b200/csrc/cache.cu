@@ -13,6 +13,7 @@
 #include "cache_common.cuh"
 #include "ctx_access.h"
 #include "kernels_cache_pages.cuh"
+#include "kernels_cache_prompt.cuh"
 #include "kernels_cache_simt.cuh"
 #include "kernels_cache_step.cuh"
 
@@ -133,9 +134,26 @@ int attend_step(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const f
   return FICOCO_OK;
 }
 template <int DIM>
+int attend_prompt(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
+  using PL = PromptPlan<DIM>;
+  CUtensorMap km, vm;
+  int rc;
+  if ((rc = code_map(ctx, c, c.k, &km)) || (rc = code_map(ctx, c, c.v, &vm))) return rc;
+  CACHE_TRY(ctx, cudaFuncSetAttribute(k_cache_prompt<DIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM));
+  const long long units = (long long)a->rows * (a->heads / c.kv) / PROMPT_ROWS + c.batch;
+  ctx_prof_tick(ctx, st, "k_cache_prompt");
+  CACHE_TRY(ctx, launch(k_cache_prompt<DIM>, dim3((unsigned)(units * c.kv)), PROMPT_THREADS, PL::SMEM, st, km, vm, c,
+                        (const __nv_bfloat16*)a->q, a->cu_rows, (__nv_bfloat16*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads,
+                        mask_rule(a), x.status, x.wait_ns));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+template <int DIM>
 int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
   if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, st);
   const long long rows = (long long)a->rows * (a->heads / c.kv);       // of all sequences, per key/value head
+  if (rows > 32ll * c.batch) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
   if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, st);
   return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, st);
 }

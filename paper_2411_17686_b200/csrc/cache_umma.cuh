@@ -72,16 +72,18 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(smem_u32(bar)) : "memory");
 }
 
-// A pair of values as NT e4m3 terms each: codes[t] holds both values' term t, the first one's in the low byte.
-template <int NT>
+// A pair of values as NT e4m3 terms each: codes[t] holds both values' term t, the first one's in the low byte.  Term t is
+// 16^t times what it stands for; with UP false the terms stand for themselves, so that products with all of them can share an
+// accumulator (the smallest step of e4m3, 2^-9, then bounds all of them).
+template <int NT, bool UP = true>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&codes)[NT]) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     codes[t] = to_e4m3x2(a, b);
     if (t + 1 < NT) {
       const float2 got = from_e4m3x2(codes[t]);
-      a = (a - got.x) * 16.f;
-      b = (b - got.y) * 16.f;
+      a = UP ? (a - got.x) * 16.f : a - got.x;
+      b = UP ? (b - got.y) * 16.f : b - got.y;
     }
   }
 }
@@ -116,7 +118,7 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
 
 // Eight elements of a query row -> NT terms at `rows` rows' distance, and what the row was divided by (NaN where the row holds
 // a NaN or an infinity).  The DIM / 8 lanes of a row are neighbours in a warp and all call this.
-template <int DIM, int NT>
+template <int DIM, int NT, bool UP = true>
 __device__ __forceinline__ float store_query(const float (&f)[8], uint32_t base, int row, int rows, int chunk8) {
   float amax = 0.f, zero = 0.f;
 #pragma unroll
@@ -130,7 +132,7 @@ __device__ __forceinline__ float store_query(const float (&f)[8], uint32_t base,
   const float s = scale_of(amax), inv = 1.0f / s;
   uint32_t c[4][NT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) split_pair<NT>(f[2 * j] * inv, f[2 * j + 1] * inv, c[j]);
+  for (int j = 0; j < 4; ++j) split_pair<NT, UP>(f[2 * j] * inv, f[2 * j + 1] * inv, c[j]);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
     st_shared8(base + swizzled<DIM>(t * rows + row, chunk8), c[0][t] | c[1][t] << 16, c[2][t] | c[3][t] << 16);

@@ -1,0 +1,434 @@
+// Attention over the 8-bit cache for many bf16 query rows per sequence (prompts and chunks of them), on the 5th-generation tensor
+// cores.
+//
+// Mathematics.  Rows of a sequence that share a key/value head are packed, 128 to a tile (row x = query x / group, head x % group of the
+// group), so that a tile reads its keys and values once for all heads of the group.  S = Q K^T per tile of 128 tokens: the keys' codes
+// as they lie in memory against two e4m3 terms of the query rows at one scale (cache_umma.cuh).  t = log2 score + log2 of the
+// page's value scale; P = 2^(t - ref) in fp16 (2^-11, where two e4m3 terms would hold 2^-8 and cost twice the conversions), the
+// values' codes converted to fp16, which is exact; the denominator sums P / value scale in fp32.  ref follows the running maximum
+// only when that has grown by more than 2^8 since (P stays below 2^8, fp16's range is 2^16), so that O is rarely rescaled.
+//
+// What bounds it: the tensor cores and the exponentials, which take about the same time: two row tiles per CTA take turns, one's
+// softmax runs under the other's products.  P lies in tensor memory in the place of the scores it came from, which spares shared
+// memory a third of its traffic (a product whose operands are both in shared memory runs at its 128 bytes per cycle).
+//
+// Roles: warps 0-3 and 4-7 softmax and epilogue of the two tiles (thread = row), warps 8-11 convert values, warp 12 TMA and page
+// scales, warp 13 MMA.  One CTA per SM and work item; a sequence's last rows, which see most, go first.
+#pragma once
+#include "cache_umma.cuh"
+
+namespace ficoco {
+
+constexpr int PROMPT_THREADS = 448;
+constexpr int PROMPT_ROWS = 256;             // rows per CTA, two tiles
+
+// tcgen05.mma kind::f16 with A (fp16) in tensor memory.
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void ctmem_ld32(uint32_t taddr, float (&f)[32]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(f);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, "
+      "%27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ctmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void ctmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t to_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint32_t f16x2_of(uint32_t codes) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+  return h;
+}
+
+template <int DIM>
+struct PromptPlan {
+  static constexpr int Q_TERM = 128 * DIM, Q_TILE = 2 * Q_TERM;      // two e4m3 terms of a row tile
+  static constexpr int CODES = CTILE * DIM;                          // keys or values of a tile of tokens
+  static constexpr int V16 = 2 * CODES;
+  static constexpr int K_ST = 3, V_ST = 2, V16_ST = 2, SC_ST = 4;
+  static constexpr int SMEM = 1024 + 2 * Q_TILE + K_ST * CODES + V_ST * CODES + V16_ST * V16;
+  static_assert(SMEM + 4096 <= 227 * 1024, "one CTA per SM");
+};
+
+template <int DIM>
+__global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
+    const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const CacheView c,
+    const __nv_bfloat16* __restrict__ q, const int* __restrict__ cu, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
+    long long q_stride, float scale_log2, int rows, int heads, const MaskRule mask, unsigned* __restrict__ status,
+    unsigned long long wait_ns) {
+  using PL = PromptPlan<DIM>;
+  constexpr int K_ST = PL::K_ST, V_ST = PL::V_ST, V16_ST = PL::V16_ST, SC_ST = PL::SC_ST;
+  extern __shared__ unsigned char prompt_raw[];
+  __shared__ uint64_t k_full[K_ST], k_empty[K_ST], v_full[V_ST], v_empty[V_ST], w_full[V16_ST], w_empty[V16_ST];
+  __shared__ uint64_t sc_full[SC_ST], sc_empty[SC_ST], q_bar, s_bar[2], p_bar[2], o_bar[2], drain_bar;
+  __shared__ uint32_t tmem_s;
+  __shared__ int dead_s;
+  __shared__ float page_scale[SC_ST][3][8];            // key scale, log2 of the value scale, 1 / value scale
+  __shared__ float q_scale[PROMPT_ROWS];
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t q_base = (smem_u32(prompt_raw) + 1023u) & ~1023u;
+  const uint32_t k_ring = q_base + 2 * PL::Q_TILE, v_ring = k_ring + K_ST * PL::CODES, w_ring = v_ring + V_ST * PL::CODES;
+  const uint32_t group = (uint32_t)(heads / c.kv);
+  if (tid == 0) {
+    for (int s = 0; s < K_ST; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
+    for (int s = 0; s < V_ST; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 4); }
+    for (int s = 0; s < V16_ST; ++s) { mbar_init(&w_full[s], 4); mbar_init(&w_empty[s], 1); }
+    for (int s = 0; s < SC_ST; ++s) { mbar_init(&sc_full[s], 1); mbar_init(&sc_empty[s], 8); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 4); mbar_init(&o_bar[s], 1); }
+    mbar_init(&q_bar, 8);
+    mbar_init(&drain_bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 13) tmem_alloc(&tmem_s, 512);
+  grid_dep_wait();
+  if (tid == 0) dead_s = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
+
+  // ---- which rows: CTA u of sequence b has rows of pair (last - u) of one head ------------------------------------------
+  const int head = blockIdx.x % c.kv;
+  const long long u = blockIdx.x / c.kv;
+  auto unit0 = [&](int s) { return (long long)max(cu[s], 0) * group / PROMPT_ROWS + s; };
+  const int b = owner_of(c.batch, unit0, u);
+  const int2 r = cache_rows(cu, b, rows, status);
+  const int n_rows = r.y - r.x, len = cache_length(c, b, status);
+  const uint32_t packed = (uint32_t)n_rows * group;                    // rows of the sequence under this head
+  const int pair = (int)((packed + PROMPT_ROWS - 1) / PROMPT_ROWS) - 1 - (int)(u - unit0(b));
+  ctc_fence_before();
+  __syncthreads();
+  ctc_fence_after();
+  grid_dep_launch();       // behind the barrier: a dependent that took this SM's TMEM first would wait for it for ever
+  const uint32_t tmem = tmem_s;
+  const bool work = pair >= 0 && u >= unit0(b) && !dead_s;
+  // ---- tiles of tokens that the rows see ----------------------------------------------------------------------------
+  const uint32_t x0 = (uint32_t)max(pair, 0) * PROMPT_ROWS;
+  auto query = [&](uint32_t x) { return (int)(min(x, packed - 1) / group); };      // of packed row x
+  int t_sink = 0, t0 = 0, nt[2] = {0, 0};
+  if (work) {
+    const int first_lo = seen(mask, len - n_rows + query(x0), len).y;
+    t0 = first_lo / CTILE;
+    t_sink = min((min(mask.sinks, first_lo) + CTILE - 1) / CTILE, t0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (x0 + 128 * t < packed) {
+        const int hi = seen(mask, len - n_rows + query(x0 + 128 * t + 127), len).z;
+        nt[t] = max(0, t_sink + (hi + CTILE - 1) / CTILE - t0);
+      }
+  }
+  const int n_tiles = max(nt[0], nt[1]);
+  auto token0 = [&](int k) { return (k < t_sink ? k : k - t_sink + t0) * CTILE; };
+  bool ok = true;                                      // the same in all lanes of a warp
+  auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
+
+  if (warp == 12) {
+    // ---------------- TMA and page scales: lane p brings page p of a tile -----------------------------------------------
+    const uint32_t bytes = (uint32_t)(c.page * DIM);
+    auto page_of = [&](int k) {                        // this lane's page of tile k, -1: none
+      const int at = k < n_tiles ? token0(k) + (lane << c.log_page) : len;
+      return lane < (CTILE >> c.log_page) && at < len ? cache_page(c, b, at >> c.log_page, 0, status) : -1;
+    };
+    int page = page_of(0), i = 0;
+    for (; i < n_tiles; ++i) {
+      const int page_next = page_of(i + 1);            // a tile ahead
+      const uint32_t load = bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, page >= 0));
+      const size_t at = (size_t)max(page, 0) * c.kv + head;
+      const float ks = page >= 0 ? c.ks[at] : 1.f, vs = page >= 0 ? c.vs[at] : 1.f;
+      const int row = (int)(at << c.log_page), ks_ = i % K_ST, vs_ = i % V_ST, cs_ = i % SC_ST;
+      if (i >= K_ST) wait(&k_empty[ks_], i / K_ST - 1);
+      if (!ok) break;
+      if (lane == 0) mbar_expect_tx(&k_full[ks_], load);
+      __syncwarp();
+      if (page >= 0) tma_rows(k_ring + ks_ * PL::CODES + lane * bytes, &kmap, row, &k_full[ks_]);
+      if (i >= SC_ST) wait(&sc_empty[cs_], i / SC_ST - 1);
+      if (ok && lane < 8) {
+        page_scale[cs_][0][lane] = ks;
+        page_scale[cs_][1][lane] = log2f(vs);
+        page_scale[cs_][2][lane] = 1.0f / vs;
+      }
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(&sc_full[cs_]);
+      if (i >= V_ST) wait(&v_empty[vs_], i / V_ST - 1);
+      if (!ok) { mbar_wait(&k_full[ks_], (uint32_t)(i / K_ST) & 1u, wait_ns); break; }
+      if (lane == 0) mbar_expect_tx(&v_full[vs_], load);
+      __syncwarp();
+      if (page >= 0) tma_rows(v_ring + vs_ * PL::CODES + lane * bytes, &vmap, row, &v_full[vs_]);
+      page = page_next;
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(status, STATUS_TIMEOUT);
+      // no copy outlives the CTA: the tiles asked for last
+      for (int k = max(0, i - K_ST); k < i; ++k) mbar_wait(&k_full[k % K_ST], (k / K_ST) & 1, wait_ns);
+      for (int k = max(0, i - V_ST); k < i; ++k) mbar_wait(&v_full[k % V_ST], (k / V_ST) & 1, wait_ns);
+    }
+  } else if (warp == 13) {
+    // ---------------- MMA: per tile of tokens, each row tile's weights times values, then its next scores ------------------
+    const uint32_t u_tmem = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    constexpr uint32_t id_s = cache_idesc(128, CTILE, 0, 0), id_o = cache_idesc(128, DIM, 0, 1);
+    auto scores = [&](int t, int i) {
+      const uint32_t qa = q_base + t * PL::Q_TILE;
+      const uint64_t kd = cache_desc<DIM>(k_ring + (i % K_ST) * PL::CODES);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t qd = cache_desc<DIM>(qa + e * PL::Q_TERM);
+#pragma unroll
+        for (int k = 0; k < DIM / 32; ++k) mma_f8(u_tmem + t * 128, qd + 2 * k, kd + 2 * k, id_s, e + k > 0);
+      }
+      mma_commit(&s_bar[t]);
+    };
+    auto sums = [&](int t, int i) {
+      // fp16 values, MN-major: 64 dimensions of 128 tokens are 16 KB, eight tokens 1 KB
+      const uint32_t w = w_ring + (i % V16_ST) * PL::V16;
+      uint64_t wd = 0;
+      wd |= (uint64_t)((w & 0x3FFFFu) >> 4);
+      wd |= (uint64_t)((CTILE * 128) >> 4) << 16;
+      wd |= (uint64_t)(1024 >> 4) << 32;
+      wd |= (uint64_t)1 << 46;
+      wd |= (uint64_t)2 << 61;
+#pragma unroll
+      for (int k = 0; k < CTILE / 16; ++k)
+        mma_f16_ts(u_tmem + 256 + t * 128, u_tmem + t * 128 + k * 8, wd + (uint64_t)(k * (2048 >> 4)), id_o, i > 0 || k > 0);
+    };
+    if (n_tiles > 0) wait(&q_bar, 0);
+    if (n_tiles > 0) wait(&k_full[0], 0);
+    if (ok && n_tiles > 0) {
+      ctc_fence_after();
+      if (nt[0] > 0) scores(0, 0);
+      if (nt[1] > 0) scores(1, 0);
+      mma_commit(&k_empty[0]);
+    }
+    for (int i = 0; ok && i < n_tiles; ++i) {
+      wait(&w_full[i % V16_ST], i / V16_ST);
+      if (ok && i + 1 < n_tiles) wait(&k_full[(i + 1) % K_ST], (i + 1) / K_ST);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (i < nt[t]) {
+          wait(&p_bar[t], i);
+          if (!ok) break;
+          ctc_fence_after();
+          sums(t, i);
+          if (i + 1 == nt[t]) mma_commit(&o_bar[t]);
+        }
+        if (i + 1 < nt[t]) scores(t, i + 1);
+      }
+      if (!ok) break;
+      mma_commit(&w_empty[i % V16_ST]);
+      if (i + 1 < n_tiles) mma_commit(&k_empty[(i + 1) % K_ST]);
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(status, STATUS_TIMEOUT);
+      mma_commit(&drain_bar);
+      mbar_wait(&drain_bar, 0, wait_ns);
+    }
+  } else if (warp >= 8) {
+    // ---------------- values: e4m3 -> fp16, thread = 16 dimensions of every (128 * 16 / DIM)-th token ---------------------
+    constexpr int CHUNKS = DIM / 16;
+    const int ct = tid - 256, ch = ct % CHUNKS;
+    for (int i = 0; ok && i < n_tiles; ++i) {
+      wait(&v_full[i % V_ST], i / V_ST);
+      if (i >= V16_ST) wait(&w_empty[i % V16_ST], i / V16_ST - 1);
+      if (!ok) break;
+      const uint32_t v = v_ring + (i % V_ST) * PL::CODES, w = w_ring + (i % V16_ST) * PL::V16 + (ch >> 2) * (CTILE * 128);
+      const int left = len - token0(i);                // tokens behind it: whatever the slot holds must not meet a weight of 0
+#pragma unroll 4
+      for (int j = ct / CHUNKS; j < CTILE; j += 128 / CHUNKS) {
+        uint32_t a[4];
+        const int sw = DIM == 128 ? ch ^ (j & 7) : ch ^ ((j >> 1) & 3);
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
+                     : "r"(v + j * DIM + sw * 16) : "memory");
+        const bool on = j < left;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) a[x] = on ? a[x] : 0u;
+        const uint32_t to = w + j * 128;
+        const int c2 = (ch & 3) * 2;                   // two 16-byte pieces of the token's 128-byte row
+        st_shared16(to + ((c2 ^ (j & 7)) << 4), f16x2_of(a[0]), f16x2_of(a[0] >> 16), f16x2_of(a[1]), f16x2_of(a[1] >> 16));
+        st_shared16(to + (((c2 + 1) ^ (j & 7)) << 4), f16x2_of(a[2]), f16x2_of(a[2] >> 16), f16x2_of(a[3]), f16x2_of(a[3] >> 16));
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(&v_empty[i % V_ST]); mbar_arrive(&w_full[i % V16_ST]); }
+    }
+    if (!ok && lane == 0) atomicOr(status, STATUS_TIMEOUT);
+  } else {
+    // ---------------- softmax: thread = row ------------------------------------------------------------------------------
+    const int t = warp >> 2, wr = warp & 3;
+    if (work) {
+      // the query rows of the CTA, 16 at a time
+      constexpr int LANES = DIM / 8, AT_ONCE = 256 / LANES, N_AT = 4;
+      const int chunk = tid % LANES;
+#pragma unroll 1
+      for (int p0 = 0; p0 < PROMPT_ROWS / AT_ONCE; p0 += N_AT) {
+        float f[N_AT][8];
+#pragma unroll
+        for (int p = 0; p < N_AT; ++p) {
+          const uint32_t x = x0 + (p0 + p) * AT_ONCE + tid / LANES;
+          const uint32_t i = x / group, g = x - i * group;
+          if (x < packed) load8(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8, f[p]);
+          else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[p][j] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < N_AT; ++p) {
+          const int row = (p0 + p) * AT_ONCE + tid / LANES;
+          const float s = store_query<DIM, 2, false>(f[p], q_base + (row >> 7) * PL::Q_TILE, row & 127, 128, chunk);
+          if (chunk == 0) q_scale[row] = s * scale_log2;
+        }
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_bar);
+    }
+    cta_sync(1, 256);                                  // the rows' scales
+    const uint32_t t_s = tmem + t * 128 + ((uint32_t)(wr * 32) << 16), t_o = t_s + 256;
+    const uint32_t x = x0 + tid;
+    const int3 see = seen(mask, len - n_rows + query(x), len);
+    const float qk = q_scale[tid];
+    const int my_nt = nt[t];
+    // a tile inside [in_lo, in_hi) is seen by every row of the warp
+    const int in_hi = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32), len).z;
+    const int in_lo = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32 + 31), len).y;
+    float ref = -CUDART_INF_F, l = 0.f;
+    for (int i = 0; i < n_tiles; ++i) {
+      const int sc = i % SC_ST;
+      if (i >= my_nt) {                                // the other tile goes on
+        wait(&sc_full[sc], i / SC_ST);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive(&sc_empty[sc]);
+        continue;
+      }
+      const int base = token0(i);
+      wait(&sc_full[sc], i / SC_ST);
+      wait(&s_bar[t], i);
+      if (!ok) break;
+      ctc_fence_after();
+      const bool edge = base < in_lo || base + CTILE > in_hi;
+      auto visible = [&](int j) { return j < see.z && (j >= see.y || j < see.x); };
+      float top = -CUDART_INF_F;
+#pragma unroll 1
+      for (int cc = 0; cc < CTILE; cc += 32) {
+        float s[32];
+        ctmem_ld32(t_s + cc, s);
+        ctmem_wait_ld();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int pg = (cc + 16 * h) >> c.log_page;
+          const float k = qk * page_scale[sc][0][pg], e = page_scale[sc][1][pg];
+          if (!edge) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, fmaf(s[16 * h + j], k, e));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, visible(base + cc + 16 * h + j) ? fmaf(s[16 * h + j], k, e) : -CUDART_INF_F);
+          }
+        }
+      }
+      // the products of the tiles before are complete: scores of this one were issued behind them
+      const bool move = top > ref + 8.f || ref == -CUDART_INF_F;
+      if (__any_sync(0xFFFFFFFFu, move)) {
+        const float to = move ? fmaxf(top, ref) : ref;
+        const float by = to == -CUDART_INF_F ? 0.f : ex2(ref - to);
+        ref = to;
+        l *= by;
+        if (i > 0) {
+#pragma unroll 1
+          for (int cc = 0; cc < DIM; cc += 16) {
+            float o[16];
+            ctmem_ld16(t_o + cc, o);
+            ctmem_wait_ld();
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(o[j] * by);
+            ctmem_st16(t_o + cc, w);
+          }
+        }
+      }
+      const float m = ref == -CUDART_INF_F ? 0.f : ref;
+#pragma unroll 1
+      for (int cc = 0; cc < CTILE; cc += 32) {
+        float s[32];
+        ctmem_ld32(t_s + cc, s);
+        ctmem_wait_ld();
+        uint32_t w[16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int pg = (cc + 16 * h) >> c.log_page;
+          const float k = qk * page_scale[sc][0][pg], e = page_scale[sc][1][pg] - m;
+          if (!edge) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[16 * h + j] = ex2(fmaf(s[16 * h + j], k, e));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[16 * h + j] = visible(base + cc + 16 * h + j) ? ex2(fmaf(s[16 * h + j], k, e)) : 0.f;
+          }
+          float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            a0 += s[16 * h + j];
+            a1 += s[16 * h + j + 1];
+            w[8 * h + j / 2] = to_f16x2(s[16 * h + j], s[16 * h + j + 1]);
+          }
+          l = fmaf(a0 + a1, base + cc + 16 * h < len ? page_scale[sc][2][pg] : 0.f, l);
+        }
+        ctmem_st16(t_s + cc / 2, w);                   // (columns whose scores have been read)
+      }
+      ctmem_wait_st();
+      ctc_fence_before();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(&p_bar[t]); mbar_arrive(&sc_empty[sc]); }
+    }
+    if (work && ok && my_nt > 0) wait(&o_bar[t], 0);
+    if (work && ok && x < packed) {
+      const uint32_t i = x / group, g = x - i * group;
+      const long long at = (long long)(r.x + (int)i) * heads + head * group + g;
+      if (lse != nullptr) lse[at] = l > 0.f || l != l ? (ref + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;
+    }
+    if (work && ok) {
+      ctc_fence_after();
+      const bool some = l > 0.f || l != l;
+      const float inv = some ? 1.0f / l : 0.f;
+      const uint32_t i = x / group, g = x - i * group;
+      __nv_bfloat16* o_at = out + ((long long)(r.x + (int)i) * heads + head * group + g) * DIM;
+#pragma unroll 1
+      for (int cc = 0; cc < DIM; cc += 16) {
+        float o[16];
+        ctmem_ld16(t_o + cc, o);
+        ctmem_wait_ld();
+        if (x < packed) {
+          uint32_t w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(some ? o[2 * j] * inv : 0.f, some ? o[2 * j + 1] * inv : 0.f);
+          *reinterpret_cast<uint4*>(o_at + cc) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(o_at + cc + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      }
+    }
+    if (!ok && lane == 0) atomicOr(status, STATUS_TIMEOUT);
+  }
+  ctc_fence_before();
+  __syncthreads();
+  if (warp == 13) tmem_free(tmem, 512);
+}
+
+}  // namespace ficoco

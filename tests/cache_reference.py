@@ -106,9 +106,10 @@ def attention(cache, q, rows, causal=True, window=0, sinks=0, scale=None):
 
     Tolerances, bf16 rows.  A softmax weight (times its page's value scale) is held as two e4m3 terms: each is off by at most
     2^-4 of what it stands for, together 2^-8; the second one's smallest step puts another 2^-22 of the largest weight on
-    every token.  A query row is two such terms of the row scaled to at most 448: exact for bf16 elements down to 2^-10 of the
-    row's largest, below that off by 2^-19 of it, which moves a score by at most ds and every weight by 2 ds (numerator and
-    denominator).  fp32 sums of 128 exact products: 2^-21 of the sum of magnitudes (measured 2^-22), exponentials and the
+    every token.  A query row is two such terms of the row scaled to between 224 and 448: exact for bf16 elements down to 2^-10
+    of the row's largest, below that off by half of the second term's smallest step, 2^-10 where both terms have one scale (many
+    rows per sequence), hence by at most 2^-10 / 224 < 2^-17 of the largest element, which moves a score by at most ds and every
+    weight by 2 ds (numerator and denominator).  With many rows weights are fp16 (2^-12, smallest step 2^-24 of the largest).  fp32 sums of 128 exact products: 2^-21 of the sum of magnitudes (measured 2^-22), exponentials and the
     other operations a few 2^-22 more.  The result is rounded to half a bf16 step, 2^-8 of it at most.
     fp32 rows: six terms, 2^-24 of the weight or better; the rest as above, and 2^-24 for the result."""
     heads, dim = q.shape[1], q.shape[2]
@@ -139,7 +140,7 @@ def attention(cache, q, rows, causal=True, window=0, sinks=0, scale=None):
                 codes = np.abs(vv) / sv[see][:, None]
                 ds = 2.0 ** -21 * s1 + 2.0 ** -21 * (1 + np.abs(s).max())
                 if bf16:
-                    ds += scale * np.abs(x).max() * np.abs(kk).sum(1).max() * 2.0 ** -18
+                    ds += scale * np.abs(x).max() * np.abs(kk).sum(1).max() * 2.0 ** -17
                 a = np.abs(vv).T @ (p / l)
                 tol[r0 + i, h] = a * ((2.0 ** -8 if bf16 else 2.0 ** -22) + 2 * ds) + \
                     (2.0 ** -22 if bf16 else 2.0 ** -27) * w.max() * codes.sum(0) + \
