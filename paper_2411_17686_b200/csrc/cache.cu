@@ -16,6 +16,7 @@
 #include "kernels_cache_prompt.cuh"
 #include "kernels_cache_simt.cuh"
 #include "kernels_cache_step.cuh"
+#include "kernels_cache_weights.cuh"
 
 using namespace ficoco;
 
@@ -158,6 +159,35 @@ int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const fi
   return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, st);
 }
 
+template <class T, int DIM, int NT, int RC>
+int weigh(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, int n_text, int first, int count,
+          float* weights, float scale_log2, cudaStream_t st) {
+  using PL = WeightPlan<DIM, NT, RC>;
+  CUtensorMap km;
+  const int rc = code_map(ctx, c, c.k, &km);
+  if (rc) return rc;
+  CACHE_TRY(ctx, cudaFuncSetAttribute(k_cache_weights<T, DIM, NT, RC>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM));
+  const int chunks = (int)(((long long)n_text * (a->heads / c.kv) + RC - 1) / RC);
+  const int tiles = (int)(((long long)first + count + CTILE - 1) / CTILE - first / CTILE);
+  // runs of tiles: enough CTAs for two waves of two per SM, where there are tiles for that
+  const long long items = (long long)chunks * c.batch * c.kv;
+  const int runs = (int)std::min<long long>(tiles, std::max(1ll, (4ll * x.num_sms + items - 1) / items));
+  const int per = (tiles + runs - 1) / runs;
+  ctx_prof_tick(ctx, st, "k_cache_weights");
+  CACHE_TRY(ctx, launch(k_cache_weights<T, DIM, NT, RC>, dim3((tiles + per - 1) / per, c.batch * c.kv, chunks), WEIGHT_THREADS, PL::SMEM, st,
+                        km, c, (const T*)a->q, a->cu_rows, a->lse, weights, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a),
+                        n_text, first, count, per, x.status, x.wait_ns));
+  ctx_prof_tick(ctx, st, nullptr);
+  ctx_set_launches(ctx, 1);
+  return FICOCO_OK;
+}
+template <int DIM>
+int weigh_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, int n_text, int first, int count,
+              float* weights, float scale_log2, cudaStream_t st) {
+  if (a->dtype == FICOCO_FP32) return weigh<float, DIM, 6, 16>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
+  return weigh<__nv_bfloat16, DIM, 2, 64>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
+}
+
 }  // namespace
 
 extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco_append_args* a, void* cuda_stream) {
@@ -229,6 +259,11 @@ extern "C" int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, 
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
   const float scale_log2 = a->scale * 1.4426950408889634f;
+  // (grid limits: 65535 CTAs each of batch x heads and row chunks; what exceeds them takes the kernel without tiles)
+  if ((long long)c.batch * c.kv <= 65535 && (long long)n_text * (a->heads / c.kv) <= 65535 * 16) {
+    if (c.dim == 128) return weigh_dim<128>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
+    if (c.dim == 64) return weigh_dim<64>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
+  }
   const dim3 grid(c.batch * n_text, a->heads);
   ctx_prof_tick(ctx, st, "k_cache_weights_simt");
   if (a->dtype == FICOCO_BF16)
