@@ -116,27 +116,27 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// Eight elements of a query row -> NT terms at `rows` rows' distance, and what the row was divided by (NaN where the row holds
-// a NaN or an infinity).  The DIM / 8 lanes of a row are neighbours in a warp and all call this.
+// What a query row is divided by, a power of two that brings it to 448 at most (NaN where the row holds a NaN or an
+// infinity), from the eight elements that each of its DIM / 8 lanes, neighbours in a warp, has.
+template <int DIM>
+__device__ __forceinline__ float query_scale(const float (&f)[8]) {
+  uint32_t top = 0;                                      // order of magnitudes as integers: infinity and NaN are the largest
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int o = DIM / 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  return top >= 0x7F800000u ? CUDART_NAN_F : scale_of(__uint_as_float(top));
+}
+// Those elements as NT terms, rows `rows` apart.
 template <int DIM, int NT, bool UP = true>
-__device__ __forceinline__ float store_query(const float (&f)[8], uint32_t base, int row, int rows, int chunk8) {
-  float amax = 0.f, zero = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) { amax = fmaxf(amax, fabsf(f[j])); zero += f[j] * 0.f; }
-#pragma unroll
-  for (int o = DIM / 16; o > 0; o >>= 1) {
-    amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-    zero += __shfl_xor_sync(0xFFFFFFFFu, zero, o);
-  }
-  if (zero != 0.f) amax = 1.f;
-  const float s = scale_of(amax), inv = 1.0f / s;
+__device__ __forceinline__ void store_query(const float (&f)[8], float scale, uint32_t base, int row, int rows, int chunk8) {
+  const float inv = scale == scale ? 1.0f / scale : 0.f;
   uint32_t c[4][NT];
 #pragma unroll
   for (int j = 0; j < 4; ++j) split_pair<NT, UP>(f[2 * j] * inv, f[2 * j + 1] * inv, c[j]);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
     st_shared8(base + swizzled<DIM>(t * rows + row, chunk8), c[0][t] | c[1][t] << 16, c[2][t] | c[3][t] << 16);
-  return zero != 0.f ? CUDART_NAN_F : s;
 }
 
 }  // namespace ficoco

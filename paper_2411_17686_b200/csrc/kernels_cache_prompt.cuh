@@ -273,27 +273,33 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     // ---------------- softmax: thread = row ------------------------------------------------------------------------------
     const int t = warp >> 2, wr = warp & 3;
     if (work) {
-      // the query rows of the CTA, 16 at a time
-      constexpr int LANES = DIM / 8, AT_ONCE = 256 / LANES, N_AT = 4;
+      // the query rows of the CTA, loads of half of them in flight at once
+      constexpr int LANES = DIM / 8, AT_ONCE = 256 / LANES, N_AT = PROMPT_ROWS / AT_ONCE / 2;
       const int chunk = tid % LANES;
 #pragma unroll 1
-      for (int p0 = 0; p0 < PROMPT_ROWS / AT_ONCE; p0 += N_AT) {
-        float f[N_AT][8];
+      for (int half = 0; half < 2; ++half) {
+        Raw8<__nv_bfloat16> raw[N_AT];
+        float scale[N_AT];
 #pragma unroll
         for (int p = 0; p < N_AT; ++p) {
-          const uint32_t x = x0 + (p0 + p) * AT_ONCE + tid / LANES;
+          const uint32_t x = x0 + (half * N_AT + p) * AT_ONCE + tid / LANES;
           const uint32_t i = x / group, g = x - i * group;
-          if (x < packed) load8(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8, f[p]);
-          else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[p][j] = 0.f;
-          }
+          if (x < packed) raw[p].load(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8);
+          else raw[p].clear();
         }
 #pragma unroll
         for (int p = 0; p < N_AT; ++p) {
-          const int row = (p0 + p) * AT_ONCE + tid / LANES;
-          const float s = store_query<DIM, 2, false>(f[p], q_base + (row >> 7) * PL::Q_TILE, row & 127, 128, chunk);
-          if (chunk == 0) q_scale[row] = s * scale_log2;
+          float f[8];
+          raw[p].get(f);
+          scale[p] = query_scale<DIM>(f);
+        }
+#pragma unroll
+        for (int p = 0; p < N_AT; ++p) {
+          const int row = (half * N_AT + p) * AT_ONCE + tid / LANES;
+          float f[8];
+          raw[p].get(f);
+          store_query<DIM, 2, false>(f, scale[p], q_base + (row >> 7) * PL::Q_TILE, row & 127, 128, chunk);
+          if (chunk == 0) q_scale[row] = scale[p] * scale_log2;
         }
       }
       fence_proxy_async();

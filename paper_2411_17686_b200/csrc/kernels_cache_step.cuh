@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     const uint32_t t_lane = tmem + ((uint32_t)(bw * 32) << 16);
     constexpr int LANES = DIM / 8, PASS_ROWS = 128 / LANES, PASSES = (RB + PASS_ROWS - 1) / PASS_ROWS;
     const int q_chunk = bt % LANES, q_row = bt / LANES;
-    float qf[PASSES][8];
+    Raw8<T> qf[PASSES];
     // rows of an item: row x of block k is head x % group of the sequence's row x / group
     auto load_q = [&](const StepSeg& g) {
 #pragma unroll
@@ -510,11 +510,8 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         const uint32_t x = (uint32_t)g.block * RB + p * PASS_ROWS + q_row;
         const int i = (int)(x / (uint32_t)group), h = g.head * group + (int)(x - (uint32_t)i * group);
         const bool on = p * PASS_ROWS + q_row < RB && i < g.s.n_rows;
-        if (on) load8(q + (long long)(g.s.row0 + i) * q_stride + (long long)h * DIM + q_chunk * 8, qf[p]);
-        else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) qf[p][j] = 0.f;
-        }
+        if (on) qf[p].load(q + (long long)(g.s.row0 + i) * q_stride + (long long)h * DIM + q_chunk * 8);
+        else qf[p].clear();
       }
     };
     auto put_q = [&](const StepSeg& g, int buf) {
@@ -522,7 +519,10 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       for (int p = 0; p < PASSES; ++p) {
         const int r = p * PASS_ROWS + q_row;
         if (PASSES * PASS_ROWS > RB && r >= RB) continue;      // (whole warps: RB is a multiple of a warp's rows)
-        const float s = store_query<DIM, NT>(qf[p], q_base + (uint32_t)buf * PL::Q_BYTES, r, RB, q_chunk);
+        float f[8];
+        qf[p].get(f);
+        const float s = query_scale<DIM>(f);
+        store_query<DIM, NT>(f, s, q_base + (uint32_t)buf * PL::Q_BYTES, r, RB, q_chunk);
         if (q_chunk == 0) q_scale[buf][r] = s * scale_log2;
       }
       if (bt < RB) {
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
           mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 16));
           const float ref = mn == -CUDART_INF_F ? 0.f : mn;
           f[w][r] = ex2(mw - ref);
-          if (w == 0) f[4][r] = ex2(m_run[p] - ref);
+          f[4][r] = ex2(m_run[p] - ref);                         // (the same from four lanes)
           m_run[p] = mn;
         }
         __syncwarp();

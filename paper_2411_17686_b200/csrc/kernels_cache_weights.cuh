@@ -20,11 +20,12 @@ struct WeightPlan {
   static constexpr int Q_BYTES = (N * DIM + 1023) / 1024 * 1024;
   static constexpr int SMEM = 1024 + STAGES * KEYS + Q_BYTES;
   static constexpr int TMEM = 2 * N <= 128 ? 128 : 256;
+  static constexpr int PER_SM = TMEM == 128 ? 4 : 2;
   static_assert(2 * N <= 256 && N % 16 == 0 && RC % 16 == 0, "two CTAs per SM");
 };
 
 template <class T, int DIM, int NT, int RC>
-__global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
+__global__ void __launch_bounds__(WEIGHT_THREADS, (WeightPlan<DIM, NT, RC>::PER_SM)) k_cache_weights(
     const __grid_constant__ CUtensorMap kmap, const CacheView c, const T* __restrict__ q, const int* __restrict__ cu,
     const float* __restrict__ lse, float* __restrict__ weights, long long q_stride, float scale_log2, int rows, int heads,
     const MaskRule mask, int n_text, int first, int count, int tiles_per_cta, unsigned* __restrict__ status,
@@ -35,9 +36,9 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
   __shared__ uint64_t k_full[NST], k_empty[NST], q_bar, s_bar[2], s_free[2], drain_bar;
   __shared__ uint32_t tmem_s;
   __shared__ int dead_s;
-  __shared__ float q_scale[RC], row_base[RC];
+  __shared__ float q_scale[RC];
+  __shared__ __align__(16) uint4 row_is[RC];           // scale of the row's scores, log2 of its denominator, where its weights lie
   __shared__ int4 row_see[RC];                         // tokens [0, x) and [y, z)
-  __shared__ long long row_at[RC];                     // where the row's weight of token 0 would lie
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t k_ring = (smem_u32(weight_raw) + 1023u) & ~1023u, q_base = k_ring + NST * PL::KEYS;
   const int group = heads / c.kv;
@@ -118,21 +119,32 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
       const int i = n_rows - n_text + m;
       return m < n_text && i >= 0 ? r.x + i : -1;
     };
-    constexpr int LANES = DIM / 8, AT_ONCE = 128 / LANES;
+    constexpr int LANES = DIM / 8, AT_ONCE = 128 / LANES, PASSES = (RC + AT_ONCE - 1) / AT_ONCE;
     const int chunk = tid % LANES;
-#pragma unroll 2
-    for (int p = 0; p < RC; p += AT_ONCE) {
-      const int x = p + tid / LANES;
-      int h;
-      const int row = row_of(x0 + x, h);
-      float f[8];
-      if (row >= 0) load8(q + (long long)row * q_stride + (long long)h * DIM + chunk * 8, f);
-      else {
+    Raw8<T> raw[PASSES];                               // all in flight at once (one after the other: 8 us for 64 rows)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+    for (int p = 0; p < PASSES; ++p) {
+      int h;
+      const int row = row_of(x0 + p * AT_ONCE + tid / LANES, h);
+      if (row >= 0) raw[p].load(q + (long long)row * q_stride + (long long)h * DIM + chunk * 8);
+      else raw[p].clear();
+    }
+    float scale[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      float f[8];
+      raw[p].get(f);
+      scale[p] = query_scale<DIM>(f);
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int x = p * AT_ONCE + tid / LANES;
+      float f[8];
+      raw[p].get(f);
+      if (x < RC) {
+        store_query<DIM, NT>(f, scale[p], q_base, x, RC, chunk);
+        if (chunk == 0) q_scale[x] = scale[p] * scale_log2;
       }
-      const float s = store_query<DIM, NT>(f, q_base, x, RC, chunk);
-      if (chunk == 0) q_scale[x] = s * scale_log2;
     }
     int in_lo = 0, in_hi = INT32_MAX;                  // tokens that all rows of the chunk see
     for (int x = tid; x < RC; x += 128) {
@@ -140,13 +152,16 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
       const int row = row_of(x0 + x, h), m = (x0 + x) / group;
       const int3 see = seen(mask, len - (r.y - row), len);
       row_see[x] = row >= 0 ? make_int4(see.x, see.y, see.z, 0) : make_int4(0, 0, 0, 0);
-      row_base[x] = row >= 0 ? lse[(long long)row * heads + h] * 1.4426950408889634f : 0.f;
-      row_at[x] = m < n_text ? (((long long)b * heads + h) * n_text + m) * count - first : -1;
+      const float base = row >= 0 ? lse[(long long)row * heads + h] * 1.4426950408889634f : 0.f;
+      row_is[x] = make_uint4(0u, __float_as_uint(base), (uint32_t)((h - head * group) * n_text + m) * (uint32_t)count, 0u);
     }
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) mbar_arrive(&q_bar);
     cta_sync(1, 128);
+    if (tid < RC) row_is[tid].x = __float_as_uint(q_scale[tid]);
+    cta_sync(1, 128);
+    float* const to = weights + ((long long)b * heads + head * group) * n_text * count - first;
     const int n_x = min(RC, n_text * group - x0);
     in_lo = row_see[n_x - 1].y;
     in_hi = row_see[0].z;                              // (rows in order of position: the first sees least ahead, the last least behind)
@@ -170,14 +185,29 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e] = u == NT - 1 ? f[e] : fmaf(s[e], 0.0625f, f[e]);
         }
+        uint32_t at[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float w = ex2(fmaf(s[e], q_scale[x + e] * ks, -row_base[x + e]));
-          if (edge) {
+          const uint4 is = row_is[x + e];
+          s[e] = ex2(fmaf(s[e], __uint_as_float(is.x) * ks, -__uint_as_float(is.y)));
+          at[e] = is.z + (uint32_t)j;
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
             const int4 see = row_see[x + e];
-            w = j < see.z && (j >= see.y || j < see.x) ? w : 0.f;
+            s[e] = j < see.z && (j >= see.y || j < see.x) ? s[e] : 0.f;
           }
-          if (mine && x + e < n_x) weights[row_at[x + e] + j] = w;
+        }
+        if (mine) {
+          if (x + 16 <= n_x) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) to[at[e]] = s[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (x + e < n_x) to[at[e]] = s[e];
+          }
         }
       }
       ctc_fence_before();
