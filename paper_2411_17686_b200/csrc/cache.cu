@@ -1,7 +1,6 @@
 // Entry points of the 8-bit paged cache (ficoco.h: append, attention, weights, copy, compact) and the host's page pool.
 #include <cuda_runtime.h>
 #include <math.h>
-#include <stdlib.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -170,14 +169,11 @@ int weigh(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_
   CACHE_TRY(ctx, cudaFuncSetAttribute(k_cache_weights<T, DIM, NT, RC>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM));
   const int chunks = (int)(((long long)n_text * (a->heads / c.kv) + RC - 1) / RC);
   const int tiles = (int)(((long long)first + count + CTILE - 1) / CTILE - first / CTILE);
-  // runs of tiles: enough CTAs for two waves of two per SM, where there are tiles for that
-  const long long items = (long long)chunks * c.batch * c.kv;
-  const int runs = (int)std::min<long long>(tiles, std::max(1ll, ((getenv("RUNS") ? atoi(getenv("RUNS")) : 4) * (long long)x.num_sms + items - 1) / items));
-  const int per = (tiles + runs - 1) / runs;
+  const long long total = (long long)chunks * c.batch * c.kv * tiles;
   ctx_prof_tick(ctx, st, "k_cache_weights");
-  CACHE_TRY(ctx, launch(k_cache_weights<T, DIM, NT, RC>, dim3((tiles + per - 1) / per, c.batch * c.kv, chunks), WEIGHT_THREADS, PL::SMEM, st,
+  CACHE_TRY(ctx, launch(k_cache_weights<T, DIM, NT, RC>, dim3((unsigned)std::min<long long>(total, 2ll * x.num_sms)), WEIGHT_THREADS, PL::SMEM, st,
                         km, c, (const T*)a->q, a->cu_rows, a->lse, weights, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a),
-                        n_text, first, count, per, x.status, x.wait_ns));
+                        n_text, first, count, tiles, chunks, x.status, x.wait_ns));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;
@@ -186,7 +182,6 @@ template <int DIM>
 int weigh_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, int n_text, int first, int count,
               float* weights, float scale_log2, cudaStream_t st) {
   if (a->dtype == FICOCO_FP32) return weigh<float, DIM, 6, 16>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
-  if (getenv("RC32")) return weigh<__nv_bfloat16, DIM, 2, 32>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
   return weigh<__nv_bfloat16, DIM, 2, 64>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
 }
 
@@ -261,10 +256,10 @@ extern "C" int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, 
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
   const float scale_log2 = a->scale * 1.4426950408889634f;
-  // (grid limits: 65535 CTAs each of batch x heads and row chunks; a head group's weights are indexed in 32 bits; what exceeds
-  // either takes the kernel without tiles)
-  if ((long long)c.batch * c.kv <= 65535 && (long long)n_text * (a->heads / c.kv) <= 65535 * 16 &&
-      (double)n_text * (a->heads / c.kv) * count + first + count < 4e9) {
+  // (items are counted and a head group's weights are indexed in 32 bits; what exceeds either takes the kernel without tiles)
+  if ((double)c.batch * c.kv * ((double)n_text * (a->heads / c.kv) / 16 + 1) < 2e9 &&
+      (double)n_text * (a->heads / c.kv) * count + first + count < 4e9 &&
+      ((double)n_text * (a->heads / c.kv) + 64) * n_text < 4e9) {
     if (c.dim == 128) return weigh_dim<128>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
     if (c.dim == 64) return weigh_dim<64>(ctx, x, c, a, n_text, first, count, weights, scale_log2, st);
   }

@@ -66,6 +66,11 @@ __device__ __forceinline__ void ctmem_ld16(uint32_t taddr, float* f) {
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr) : "memory");
 }
+// An arrival that promises nothing about memory: for handing back what was only read (tensor memory behind its wait), by
+// threads with global stores in flight.  The ordinary, releasing arrival waits for those, 900 cycles and more.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 // Rows of codes, one box of page_size tokens, to shared memory in the swizzle that the tensor map names.
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -86,6 +91,12 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&codes)[N
       b = UP ? (b - got.y) * 16.f : b - got.y;
     }
   }
+}
+__device__ __forceinline__ float2 mul2(const float2& a, const float2& b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d)
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
+  return reinterpret_cast<const float2&>(d);
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
