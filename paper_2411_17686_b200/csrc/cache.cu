@@ -88,6 +88,22 @@ MaskRule mask_rule(const ficoco_attention_args* a) {
     if (e__ != cudaSuccess) return ctx_cuda_error((ctx), e__); \
   } while (0)
 
+// Log2 of the threads of a team that holds `vectors` vectors, `held` each: 32 to half a CTA (two teams at least, a head's keys and
+// values).
+int team_log(int vectors, int held) {
+  int l = 5;
+  while (l < PAGE_LOG - 1 && (held << l) < vectors) ++l;
+  return l;
+}
+
+template <class T, int HELD>
+cudaError_t append(const CacheView& c, const ficoco_append_args* a, int rows_held, unsigned* status, cudaStream_t st) {
+  const int log_team = team_log(rows_held * c.dim / 8, HELD);
+  const dim3 grid(a->rows / c.page + 2 * c.batch, ((2 * c.kv << log_team) + PAGE_THREADS - 1) / PAGE_THREADS);
+  return launch(k_cache_append<T, HELD>, grid, PAGE_THREADS, 0, st, c, (const T*)a->k, (const T*)a->v, a->cu_rows, a->k_stride, a->v_stride,
+                a->rows, log_team, status);
+}
+
 // Tensor maps over the code arrays: rows of head_dim bytes, boxes of a page, the swizzle of a row's width.
 typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -200,14 +216,12 @@ extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, c
   CACHE_TRY(ctx, cudaSetDevice(x.device));
   ctx_set_launches(ctx, 0);
   if (a->rows == 0) return FICOCO_OK;
-  const dim3 grid(a->rows / c.page + 2 * c.batch, c.kv);
   ctx_prof_tick(ctx, st, "k_cache_append");
-  if (a->dtype == FICOCO_BF16)
-    CACHE_TRY(ctx, launch(k_cache_append<__nv_bfloat16>, grid, PAGE_THREADS, 0, st, c, (const __nv_bfloat16*)a->k,
-                          (const __nv_bfloat16*)a->v, a->cu_rows, a->k_stride, a->v_stride, a->rows, x.status));
-  else
-    CACHE_TRY(ctx, launch(k_cache_append<float>, grid, PAGE_THREADS, 0, st, c, (const float*)a->k, (const float*)a->v,
-                          a->cu_rows, a->k_stride, a->v_stride, a->rows, x.status));
+  // teams that hold a full page, or, where few rows come per sequence, four rows (longer ones are read twice)
+  const bool few = a->rows <= 4ll * c.batch, bf16 = a->dtype == FICOCO_BF16;
+  CACHE_TRY(ctx, few ? (bf16 ? append<__nv_bfloat16, STEP_HELD>(c, a, 4, x.status, st) : append<float, STEP_HELD>(c, a, 4, x.status, st))
+                     : (bf16 ? append<__nv_bfloat16, APPEND_HELD>(c, a, c.page, x.status, st)
+                             : append<float, APPEND_HELD>(c, a, c.page, x.status, st)));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;
@@ -309,10 +323,12 @@ extern "C" int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, 
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
-  const dim3 grid((unsigned)(((long long)a->n_kept + (long long)c.batch * a->first) / c.page + 2 * c.batch), c.kv);
+  const int log_team = team_log(c.page * c.dim / 16, COMPACT_HELD);
+  const dim3 grid((unsigned)(((long long)a->n_kept + (long long)c.batch * a->first) / c.page + 2 * c.batch),
+                  ((2 * c.kv << log_team) + PAGE_THREADS - 1) / PAGE_THREADS);
   ctx_prof_tick(ctx, st, "k_cache_compact");
   CACHE_TRY(ctx, launch(k_cache_compact, grid, PAGE_THREADS, 0, st, c, a->to_table, a->kept, a->cu_kept, a->lengths_out,
-                        a->to_stride, a->to_pages, a->n_kept, a->first, x.status));
+                        a->to_stride, a->to_pages, a->n_kept, a->first, log_team, x.status));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;

@@ -1,37 +1,47 @@
 // Kernels that write pages of the 8-bit cache: append, compact, copy.
 //
-// Append and compact share one shape.  A CTA owns one page and one key/value head; its lower half of threads works on the
-// keys, the upper half on the values.  It reads its rows once for the largest magnitude, settles the scale (a power of two,
-// so that the division is exact and the only rounding is the one to e4m3), and reads them again, now from L1 or L2,
-// for the codes.  Which sequence a CTA belongs to follows from cu_rows and the lengths on the device; the host sizes the grid
-// for the most pages that so many rows can touch (rows / page + 2 per sequence), the CTAs beyond return at once.
+// Append and compact share one shape.  A CTA owns one page and some of its key/value heads; a team of threads (a power of two,
+// a warp at least, sized by the host so that its part of the page stays in registers) works on the keys or the values of one head.
+// It reads its rows once for the largest magnitude, settles the scale (a power of two, so that the division is exact and the only
+// rounding is the one to e4m3) and converts what it holds.  Which sequence a CTA belongs to follows from cu_rows and the
+// lengths on the device; the host sizes the grid for the most pages that so many rows can touch (rows / page + 2 per sequence), the
+// CTAs beyond return at once.
+// What bounds them: HBM on prompts; the chain of lookups (sequence, length, page, old scale) on single tokens.
 #pragma once
 #include "cache_common.cuh"
 
 namespace ficoco {
 
-constexpr int PAGE_THREADS = 256;
-constexpr int PAGE_HALF = PAGE_THREADS / 2;
+constexpr int PAGE_LOG = 8, PAGE_THREADS = 1 << PAGE_LOG;
+// Vectors that a thread keeps between the two passes; more are read again.  Four CTAs of 64 registers a thread per SM, and as much as
+// those take without spilling: 16 prompts of 640 rows and 32 heads 58 us with eight, 78 with four; single tokens of 64 sequences
+// 6.2 us with eight (most of them empty), 4.3 with four; 48 gathered sequences 479 with eight, 193 with four.
+constexpr int APPEND_HELD = 8, STEP_HELD = 4, COMPACT_HELD = 4;
 
-// Largest of `v` over the PAGE_HALF threads of each half of the CTA (all values >= 0).
-__device__ __forceinline__ float half_max(float v, float (&warp_max)[PAGE_THREADS / 32]) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = v;
+// Largest of `v` over the team of this thread (all values >= 0).
+__device__ __forceinline__ float team_max(float v, int team_warps, float (&warp_max)[PAGE_THREADS / 32]) {
+  const int warp = threadIdx.x >> 5;
+  v = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v)));
+  if (team_warps == 1) return v;
+  __syncthreads();                        // (what an earlier call left has been read)
+  if ((threadIdx.x & 31) == 0) warp_max[warp] = v;
   __syncthreads();
-  const float* m = warp_max + (threadIdx.x >= PAGE_HALF ? PAGE_HALF / 32 : 0);
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+  const int w0 = warp & ~(team_warps - 1);
+  v = warp_max[w0];
+  for (int w = 1; w < team_warps; ++w) v = fmaxf(v, warp_max[w0 + w]);
+  return v;
 }
 
-template <class T>
-__global__ void __launch_bounds__(PAGE_THREADS) k_cache_append(const CacheView c, const T* __restrict__ k, const T* __restrict__ v,
+template <class T, int HELD>
+__global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_HELD ? 4 : 2)) k_cache_append(const CacheView c, const T* __restrict__ k, const T* __restrict__ v,
                                                               const int* __restrict__ cu, long long k_stride, long long v_stride,
-                                                              int rows, unsigned* __restrict__ status) {
+                                                              int rows, int log_team, unsigned* __restrict__ status) {
   __shared__ float warp_max[PAGE_THREADS / 32];
-  __shared__ int poisoned[128];
+  __shared__ unsigned poisoned[PAGE_THREADS / 64][4];          // per head of the CTA: rows of the page that hold a NaN or an infinity
   grid_dep_wait();
   grid_dep_launch();
-  const int u = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+  const int u = blockIdx.x, tid = threadIdx.x;
+  if (tid < PAGE_THREADS / 64 * 4) poisoned[tid >> 2][tid & 3] = 0u;
   const int b = owner_of(c.batch, [&](int s) { return (long long)(max(cu[s], 0) >> c.log_page) + 2 * s; }, u);
   const int2 r = cache_rows(cu, b, rows, status);
   const int n = r.y - r.x, len = cache_length(c, b, status), start = len - n;
@@ -45,46 +55,68 @@ __global__ void __launch_bounds__(PAGE_THREADS) k_cache_append(const CacheView c
   const int s0 = max(from - (pi << c.log_page), 0), s1 = min(len - (pi << c.log_page), c.page);
   const int row0 = r.x + ((pi << c.log_page) + s0 - start);
 
-  const bool is_v = tid >= PAGE_HALF;
-  const int ht = tid & (PAGE_HALF - 1);
-  const T* src = (is_v ? v : k) + (long long)row0 * (is_v ? v_stride : k_stride) + head * c.dim;
+  const int team = 1 << log_team, mine = tid >> log_team, lane = tid & (team - 1);
+  const int pair = (blockIdx.y << (PAGE_LOG - log_team)) + mine, head = pair >> 1;       // (head, keys or values); two teams of a head side by side
+  const bool is_v = pair & 1, on = head < c.kv;
+  const int vecs = c.dim >> 3, total = on ? (s1 - s0) * vecs : 0;                 // vectors of eight elements
   const long long stride = is_v ? v_stride : k_stride;
-  const size_t at = (size_t)page * c.kv + head;
+  const T* src = (is_v ? v : k) + (long long)row0 * stride + (on ? head : 0) * c.dim;
+  const size_t at = (size_t)page * c.kv + (on ? head : 0);
   uint8_t* dst = (is_v ? c.v : c.k) + (at << c.log_page) * c.dim;
   float* scale = (is_v ? c.vs : c.ks) + at;
   const float old = s0 > 0 ? *scale : 0.f;
-  const int vecs = c.dim >> 3, total = (s1 - s0) * vecs;       // vectors of eight elements
+  const int dim_log = 31 - __clz(vecs), row_of_pow2 = (vecs & (vecs - 1)) == 0;    // (a division per vector otherwise)
+  auto row_of = [&](int i) { return row_of_pow2 ? i >> dim_log : i / vecs; };
+  auto from_row = [&](int i, int row) { return src + row * stride + (i - row * vecs) * 8; };
 
-  if (tid < s1 - s0) poisoned[tid] = 0;
-  __syncthreads();
-  float amax = 0.f;
-  bool bad = false;
-  for (int i = ht; i < total; i += PAGE_HALF) {
-    const int row = i / vecs;
-    float f[8];
-    load8(src + row * stride + (i - row * vecs) * 8, f);
-    float m = 0.f, zero = 0.f;
+  Raw8<T> held[HELD];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { m = fmaxf(m, fabsf(f[j])); zero += f[j] * 0.f; }    // (NaN * 0 and infinity * 0 are NaN)
-    if (zero != 0.f) { poisoned[row] = 1; bad = true; }
-    amax = fmaxf(amax, m);
+  for (int x = 0; x < HELD; ++x) {
+    const int i = lane + (x << log_team);
+    if (i < total) held[x].load(from_row(i, row_of(i)));
+    else held[x].clear();
   }
-  if (__syncthreads_or(bad)) {                                 // rare: once more without the rows that do not count
-    amax = 0.f;
-    for (int i = ht; i < total; i += PAGE_HALF) {
-      const int row = i / vecs;
-      if (poisoned[row]) continue;
-      float f[8];
-      load8(src + row * stride + (i - row * vecs) * 8, f);
+  uint32_t top = 0;                       // order of magnitudes as integers: infinity and NaN are the largest
+  bool bad = false;
+  auto look = [&](const Raw8<T>& raw, int i) {
+    float f[8];
+    raw.get(f);
+    uint32_t m = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+    if (m >= 0x7F800000u) {
+      const int row = row_of(i);
+      atomicOr(&poisoned[mine >> 1][row >> 5], 1u << (row & 31));
+      bad = true;
+    }
+    top = max(top, m);
+  };
+#pragma unroll
+  for (int x = 0; x < HELD; ++x) look(held[x], lane + (x << log_team));
+  for (int i = lane + (HELD << log_team); i < total; i += team) {
+    Raw8<T> raw;
+    raw.load(from_row(i, row_of(i)));
+    look(raw, i);
+  }
+  const bool any_bad = __syncthreads_or(bad);
+  auto is_bad = [&](int row) { return (poisoned[mine >> 1][row >> 5] >> (row & 31) & 1u) != 0; };
+  if (any_bad) {                          // rare: once more without the rows that do not count
+    top = 0;
+    for (int i = lane; i < total; i += team) {
+      const int row = row_of(i);
+      if (is_bad(row)) continue;
+      float f[8];
+      load8(from_row(i, row), f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
     }
   }
-  amax = half_max(amax, warp_max);
+  const float amax = team_max(__uint_as_float(top), team >> 5, warp_max);
+  if (!on) return;
   const float s = fmaxf(scale_of(amax), old), inv = 1.0f / s;
-  if (s0 > 0 && s > old) {                                     // the older codes of the page move to the larger scale
+  if (s0 > 0 && s > old) {                // the older codes of the page move to the larger scale
     const float f = old * inv;
-    for (int i = ht; i < s0 * vecs; i += PAGE_HALF) {
+    for (int i = lane; i < s0 * vecs; i += team) {
       uint2* p = reinterpret_cast<uint2*>(dst) + i;
       float x[8];
       from_e4m3x8(*p, x);
@@ -94,36 +126,44 @@ __global__ void __launch_bounds__(PAGE_THREADS) k_cache_append(const CacheView c
     }
   }
   uint2* out = reinterpret_cast<uint2*>(dst) + s0 * vecs;
-  for (int i = ht; i < total; i += PAGE_HALF) {
-    const int row = i / vecs;
+  auto put = [&](const Raw8<T>& raw, int i) {
     float f[8];
-    load8(src + row * stride + (i - row * vecs) * 8, f);
+    raw.get(f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] *= inv;
     uint2 codes = to_e4m3x8(f);
-    if (poisoned[row]) codes = is_v ? make_uint2(0u, 0u) : make_uint2(E4M3_NAN4, E4M3_NAN4);
+    if (any_bad && is_bad(row_of(i))) codes = is_v ? make_uint2(0u, 0u) : make_uint2(E4M3_NAN4, E4M3_NAN4);
     out[i] = codes;
+  };
+#pragma unroll
+  for (int x = 0; x < HELD; ++x) {
+    const int i = lane + (x << log_team);
+    if (i < total) put(held[x], i);
   }
-  if (ht == 0) *scale = s;
+  for (int i = lane + (HELD << log_team); i < total; i += team) {
+    Raw8<T> raw;
+    raw.load(from_row(i, row_of(i)));
+    put(raw, i);
+  }
+  if (lane == 0) *scale = s;
 }
 
-__global__ void __launch_bounds__(PAGE_THREADS) k_cache_compact(const CacheView c, const int* __restrict__ to_table,
+__global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheView c, const int* __restrict__ to_table,
                                                                const int* __restrict__ kept, const int* __restrict__ cu,
                                                                int* __restrict__ lengths_out, long long to_stride,
-                                                               int to_pages, int n_kept, int first,
+                                                               int to_pages, int n_kept, int first, int log_team,
                                                                unsigned* __restrict__ status) {
   __shared__ float warp_max[PAGE_THREADS / 32];
-  __shared__ size_t row_at[128];                               // code offset of each row of the page in the pool
-  __shared__ float row_scale[2][128];
+  __shared__ int2 row_from[128];                               // page and slot of each row of the new page
   grid_dep_wait();
   grid_dep_launch();
-  const int u = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+  const int u = blockIdx.x, tid = threadIdx.x;
   auto unit0 = [&](int s) { return ((max(cu[s], 0) + (long long)s * first) >> c.log_page) + 2 * s; };
   const int b = owner_of(c.batch, unit0, u);
   const int2 r = cache_rows(cu, b, n_kept, status);
   const int len = cache_length(c, b, status), front = min(first, len), total_rows = front + (r.y - r.x);
   const int pi = (int)(u - unit0(b));
-  if (pi == 0 && head == 0 && tid == 0 && lengths_out != nullptr) lengths_out[b] = total_rows;
+  if (pi == 0 && blockIdx.y == 0 && tid == 0 && lengths_out != nullptr) lengths_out[b] = total_rows;
   const int s1 = min(total_rows - (pi << c.log_page), c.page);
   if (pi < 0 || s1 <= 0) return;
   int page = -1;
@@ -140,42 +180,79 @@ __global__ void __launch_bounds__(PAGE_THREADS) k_cache_compact(const CacheView 
       pos = front + e;
       if (e < 0 || pos >= len) { atomicOr(status, STATUS_CACHE); pos = 0; }
     }
-    // a sequence without tokens has nothing to gather, not even token 0: zeros
-    const int sp = len > 0 ? cache_page(c, b, pos >> c.log_page, 0, status) : 0;
-    const size_t at = (size_t)sp * c.kv + head;
-    row_at[tid] = ((at << c.log_page) + (pos & (c.page - 1))) * c.dim;
-    row_scale[0][tid] = len > 0 ? c.ks[at] : 0.f;
-    row_scale[1][tid] = len > 0 ? c.vs[at] : 0.f;
+    // a sequence without tokens has nothing to gather, not even token 0: zeros (page -1)
+    row_from[tid] = make_int2(len > 0 ? cache_page(c, b, pos >> c.log_page, 0, status) : -1, pos & (c.page - 1));
   }
   __syncthreads();
-  const bool is_v = tid >= PAGE_HALF;
-  const int ht = tid & (PAGE_HALF - 1);
+  const int team = 1 << log_team, mine = tid >> log_team, lane = tid & (team - 1);
+  const int pair = (blockIdx.y << (PAGE_LOG - log_team)) + mine, head = pair >> 1;
+  const bool is_v = pair & 1, on = head < c.kv;
+  const int vecs = c.dim >> 4, total = on ? s1 * vecs : 0;      // vectors of 16 codes
   const uint8_t* src = is_v ? c.v : c.k;
-  const float* rs = row_scale[is_v ? 1 : 0];
-  const size_t at = (size_t)page * c.kv + head;
-  const int vecs = c.dim >> 3, total = s1 * vecs;
-  float amax = 0.f;
-  for (int i = ht; i < total; i += PAGE_HALF) {
-    const int row = i / vecs;
-    float f[8];
-    from_e4m3x8(*reinterpret_cast<const uint2*>(src + row_at[row] + (i - row * vecs) * 8), f);
+  const float* scales = is_v ? c.vs : c.ks;
+  const int dim_log = 31 - __clz(vecs), row_of_pow2 = (vecs & (vecs - 1)) == 0;
+  auto fetch = [&](int i, uint4& codes, float& s) {
+    const int row = row_of_pow2 ? i >> dim_log : i / vecs;
+    const int2 f = row_from[row];
+    const size_t at = (size_t)max(f.x, 0) * c.kv + head;
+    codes = *reinterpret_cast<const uint4*>(src + ((at << c.log_page) + f.y) * c.dim + (i - row * vecs) * 16);
+    s = f.x >= 0 ? scales[at] : 0.f;
+  };
+  auto look = [&](const uint4& u4, float s) {
+    const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
     float m = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[j]));     // (a NaN key counts for nothing)
-    amax = fmaxf(amax, m * rs[row]);
-  }
-  amax = half_max(amax, warp_max);
-  const float s = scale_of(amax), inv = 1.0f / s;
-  uint2* out = reinterpret_cast<uint2*>((is_v ? c.v : c.k) + (at << c.log_page) * c.dim);
-  for (int i = ht; i < total; i += PAGE_HALF) {
-    const int row = i / vecs;
-    float f[8];
-    from_e4m3x8(*reinterpret_cast<const uint2*>(src + row_at[row] + (i - row * vecs) * 8), f);
+    for (int k = 0; k < 4; ++k) {
+      const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
+      m = fmaxf(fmaxf(m, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(d.x), fabsf(d.y)));       // (a NaN key counts for nothing)
+    }
+    return m * s;
+  };
+  uint4 held[COMPACT_HELD];
+  float hs[COMPACT_HELD];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = (f[j] * rs[row]) * inv; // exact: powers of two (their quotient alone can overflow)
-    out[i] = to_e4m3x8(f);
+  for (int x = 0; x < COMPACT_HELD; ++x) {
+    const int i = lane + (x << log_team);
+    held[x] = make_uint4(0u, 0u, 0u, 0u);
+    hs[x] = 0.f;
+    if (i < total) fetch(i, held[x], hs[x]);
   }
-  if (ht == 0) (is_v ? c.vs : c.ks)[at] = s;
+  float amax = 0.f;
+#pragma unroll
+  for (int x = 0; x < COMPACT_HELD; ++x) amax = fmaxf(amax, look(held[x], hs[x]));
+  for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
+    uint4 u4;
+    float s;
+    fetch(i, u4, s);
+    amax = fmaxf(amax, look(u4, s));
+  }
+  amax = team_max(amax, team >> 5, warp_max);
+  if (!on) return;
+  const size_t at = (size_t)page * c.kv + head;
+  const float s = scale_of(amax), inv = 1.0f / s;
+  uint4* out = reinterpret_cast<uint4*>((is_v ? c.v : c.k) + (at << c.log_page) * c.dim);
+  auto put = [&](int i, const uint4& u4, float by) {
+    const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {                              // exact: powers of two (their quotient alone can overflow)
+      const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
+      o[k] = to_e4m3x2(a.x * by * inv, a.y * by * inv) | to_e4m3x2(d.x * by * inv, d.y * by * inv) << 16;
+    }
+    out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+  };
+#pragma unroll
+  for (int x = 0; x < COMPACT_HELD; ++x) {
+    const int i = lane + (x << log_team);
+    if (i < total) put(i, held[x], hs[x]);
+  }
+  for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
+    uint4 u4;
+    float by;
+    fetch(i, u4, by);
+    put(i, u4, by);
+  }
+  if (lane == 0) (is_v ? c.vs : c.ks)[at] = s;
 }
 
 // One CTA per page pair and part of the page; `words` 16-byte words of codes per page, keys and values alike.
