@@ -12,14 +12,14 @@
 // softmax runs under the other's products.  P lies in tensor memory in the place of the scores it came from, which spares shared
 // memory a third of its traffic (a product whose operands are both in shared memory runs at its 128 bytes per cycle).
 //
-// Roles: warps 0-3 and 4-7 softmax and epilogue of the two tiles (thread = row), warps 8-11 convert values, warp 12 TMA and page
-// scales, warp 13 MMA.  One CTA per SM and work item; a sequence's last rows, which see most, go first.
+// Roles: warps 0-7 and 8-15 softmax and epilogue of the two tiles (thread = row and half of the tokens, scores in registers; a warp and
+// its partner exchange maxima), warps 16 and 17 convert values, warp 18 TMA and page scales, warp 19 MMA.  One CTA per SM and work item; a sequence's last rows, which see most, go first.
 #pragma once
 #include "cache_umma.cuh"
 
 namespace ficoco {
 
-constexpr int PROMPT_THREADS = 448;
+constexpr int PROMPT_THREADS = 640;
 constexpr int PROMPT_ROWS = 256;             // rows per CTA, two tiles
 
 // tcgen05.mma kind::f16 with A (fp16) in tensor memory.
@@ -49,6 +49,17 @@ __device__ __forceinline__ void ctmem_st16(uint32_t taddr, const uint32_t (&r)[1
       "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void ctmem_st32(uint32_t taddr, const float* f) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(f);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+      "%28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31]) : "memory");
 }
 __device__ __forceinline__ void ctmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t to_f16x2(float lo, float hi) {
@@ -87,6 +98,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   __shared__ int dead_s;
   __shared__ float page_scale[SC_ST][3][8];            // key scale, log2 of the value scale, 1 / value scale
   __shared__ float q_scale[PROMPT_ROWS];
+  __shared__ float half_s[2][PROMPT_ROWS];             // per half of the tokens: a tile's maxima, in the end the denominators
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t q_base = (smem_u32(prompt_raw) + 1023u) & ~1023u;
@@ -94,15 +106,15 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   const uint32_t group = (uint32_t)(heads / c.kv);
   if (tid == 0) {
     for (int s = 0; s < K_ST; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
-    for (int s = 0; s < V_ST; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 4); }
-    for (int s = 0; s < V16_ST; ++s) { mbar_init(&w_full[s], 4); mbar_init(&w_empty[s], 1); }
-    for (int s = 0; s < SC_ST; ++s) { mbar_init(&sc_full[s], 1); mbar_init(&sc_empty[s], 8); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 4); mbar_init(&o_bar[s], 1); }
-    mbar_init(&q_bar, 8);
+    for (int s = 0; s < V_ST; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 2); }
+    for (int s = 0; s < V16_ST; ++s) { mbar_init(&w_full[s], 2); mbar_init(&w_empty[s], 1); }
+    for (int s = 0; s < SC_ST; ++s) { mbar_init(&sc_full[s], 1); mbar_init(&sc_empty[s], 16); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 8); mbar_init(&o_bar[s], 1); }
+    mbar_init(&q_bar, 16);
     mbar_init(&drain_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 13) tmem_alloc(&tmem_s, 512);
+  if (warp == 19) tmem_alloc(&tmem_s, 512);
   grid_dep_wait();
   if (tid == 0) dead_s = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
 
@@ -141,7 +153,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   bool ok = true;                                      // the same in all lanes of a warp
   auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
 
-  if (warp == 12) {
+  if (warp == 18) {
     // ---------------- TMA and page scales: lane p brings page p of a tile -----------------------------------------------
     const uint32_t bytes = (uint32_t)(c.page * DIM);
     auto page_of = [&](int k) {                        // this lane's page of tile k, -1: none
@@ -181,7 +193,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
       for (int k = max(0, i - K_ST); k < i; ++k) mbar_wait(&k_full[k % K_ST], (k / K_ST) & 1, wait_ns);
       for (int k = max(0, i - V_ST); k < i; ++k) mbar_wait(&v_full[k % V_ST], (k / V_ST) & 1, wait_ns);
     }
-  } else if (warp == 13) {
+  } else if (warp == 19) {
     // ---------------- MMA: per tile of tokens, each row tile's weights times values, then its next scores ------------------
     const uint32_t u_tmem = __shfl_sync(0xFFFFFFFFu, tmem, 0);
     constexpr uint32_t id_s = cache_idesc(128, CTILE, 0, 0), id_o = cache_idesc(128, DIM, 0, 1);
@@ -240,10 +252,10 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
       mma_commit(&drain_bar);
       mbar_wait(&drain_bar, 0, wait_ns);
     }
-  } else if (warp >= 8) {
-    // ---------------- values: e4m3 -> fp16, thread = 16 dimensions of every (128 * 16 / DIM)-th token ---------------------
+  } else if (warp >= 16) {
+    // ---------------- values: e4m3 -> fp16, thread = 16 dimensions of every (64 * 16 / DIM)-th token ---------------------
     constexpr int CHUNKS = DIM / 16;
-    const int ct = tid - 256, ch = ct % CHUNKS;
+    const int ct = tid - 512, ch = ct % CHUNKS;
     for (int i = 0; ok && i < n_tiles; ++i) {
       wait(&v_full[i % V_ST], i / V_ST);
       if (i >= V16_ST) wait(&w_empty[i % V16_ST], i / V16_ST - 1);
@@ -251,7 +263,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
       const uint32_t v = v_ring + (i % V_ST) * PL::CODES, w = w_ring + (i % V16_ST) * PL::V16 + (ch >> 2) * (CTILE * 128);
       const int left = len - token0(i);                // tokens behind it: whatever the slot holds must not meet a weight of 0
 #pragma unroll 4
-      for (int j = ct / CHUNKS; j < CTILE; j += 128 / CHUNKS) {
+      for (int j = ct / CHUNKS; j < CTILE; j += 64 / CHUNKS) {
         uint32_t a[4];
         const int sw = DIM == 128 ? ch ^ (j & 7) : ch ^ ((j >> 1) & 3);
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
@@ -270,53 +282,54 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     }
     if (!ok && lane == 0) atomicOr(status, STATUS_TIMEOUT);
   } else {
-    // ---------------- softmax: thread = row ------------------------------------------------------------------------------
-    const int t = warp >> 2, wr = warp & 3;
+    // ---------------- softmax: thread = row and half of the tokens ---------------------------------------------------------
+    const int t = warp >> 3, half = warp >> 2 & 1, wr = warp & 3, row = t * 128 + wr * 32 + lane, pair_bar = 1 + t * 4 + wr;
     if (work) {
-      // the query rows of the CTA, loads of half of them in flight at once
-      constexpr int LANES = DIM / 8, AT_ONCE = 256 / LANES, N_AT = PROMPT_ROWS / AT_ONCE / 2;
+      // the query rows of the CTA, all loads in flight at once
+      constexpr int LANES = DIM / 8, AT_ONCE = 512 / LANES, N_AT = PROMPT_ROWS / AT_ONCE;
       const int chunk = tid % LANES;
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        Raw8<__nv_bfloat16> raw[N_AT];
-        float scale[N_AT];
+      Raw8<__nv_bfloat16> raw[N_AT];
+      float scale[N_AT];
 #pragma unroll
-        for (int p = 0; p < N_AT; ++p) {
-          const uint32_t x = x0 + (half * N_AT + p) * AT_ONCE + tid / LANES;
-          const uint32_t i = x / group, g = x - i * group;
-          if (x < packed) raw[p].load(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8);
-          else raw[p].clear();
-        }
+      for (int p = 0; p < N_AT; ++p) {
+        const uint32_t x = x0 + p * AT_ONCE + tid / LANES;
+        const uint32_t i = x / group, g = x - i * group;
+        if (x < packed) raw[p].load(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8);
+        else raw[p].clear();
+      }
 #pragma unroll
-        for (int p = 0; p < N_AT; ++p) {
-          float f[8];
-          raw[p].get(f);
-          scale[p] = query_scale<DIM>(f);
-        }
+      for (int p = 0; p < N_AT; ++p) {
+        float f[8];
+        raw[p].get(f);
+        scale[p] = query_scale<DIM>(f);
+      }
 #pragma unroll
-        for (int p = 0; p < N_AT; ++p) {
-          const int row = (half * N_AT + p) * AT_ONCE + tid / LANES;
-          float f[8];
-          raw[p].get(f);
-          store_query<DIM, 2, false>(f, scale[p], q_base + (row >> 7) * PL::Q_TILE, row & 127, 128, chunk);
-          if (chunk == 0) q_scale[row] = scale[p] * scale_log2;
-        }
+      for (int p = 0; p < N_AT; ++p) {
+        const int x = p * AT_ONCE + tid / LANES;
+        float f[8];
+        raw[p].get(f);
+        store_query<DIM, 2, false>(f, scale[p], q_base + (x >> 7) * PL::Q_TILE, x & 127, 128, chunk);
+      }
+      if (chunk == 0) {
+#pragma unroll
+        for (int p = 0; p < N_AT; ++p) q_scale[p * AT_ONCE + tid / LANES] = scale[p] * scale_log2;
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_bar);
     }
-    cta_sync(1, 256);                                  // the rows' scales
-    const uint32_t t_s = tmem + t * 128 + ((uint32_t)(wr * 32) << 16), t_o = t_s + 256;
-    const uint32_t x = x0 + tid;
+    cta_sync(9, 512);                                  // the rows' scales
+    const uint32_t t_s = tmem + t * 128 + ((uint32_t)(wr * 32) << 16), t_o = t_s + 256 + half * (DIM / 2);
+    const uint32_t x = x0 + row;
     const int3 see = seen(mask, len - n_rows + query(x), len);
-    const float qk = q_scale[tid];
+    const float qk = q_scale[row];
     const int my_nt = nt[t];
     // a tile inside [in_lo, in_hi) is seen by every row of the warp
     const int in_hi = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32), len).z;
     const int in_lo = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32 + 31), len).y;
     float ref = -CUDART_INF_F, l = 0.f;
-    for (int i = 0; i < n_tiles; ++i) {
+    bool alive = true;                                 // the same in a warp and its partner, who share a barrier per tile
+    for (int i = 0; alive && i < n_tiles; ++i) {
       const int sc = i % SC_ST;
       if (i >= my_nt) {                                // the other tile goes on
         wait(&sc_full[sc], i / SC_ST);
@@ -324,32 +337,35 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
         if (lane == 0) mbar_arrive(&sc_empty[sc]);
         continue;
       }
-      const int base = token0(i);
+      const int base = token0(i) + half * 64;
       wait(&sc_full[sc], i / SC_ST);
       wait(&s_bar[t], i);
-      if (!ok) break;
       ctc_fence_after();
-      const bool edge = base < in_lo || base + CTILE > in_hi;
-      auto visible = [&](int j) { return j < see.z && (j >= see.y || j < see.x); };
+      float s[64];
+      ctmem_ld32(t_s + half * 64, *reinterpret_cast<float (*)[32]>(s));
+      ctmem_ld32(t_s + half * 64 + 32, *reinterpret_cast<float (*)[32]>(s + 32));
+      ctmem_wait_ld();
       float top = -CUDART_INF_F;
-#pragma unroll 1
-      for (int cc = 0; cc < CTILE; cc += 32) {
-        float s[32];
-        ctmem_ld32(t_s + cc, s);
-        ctmem_wait_ld();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int pg = (cc + 16 * h) >> c.log_page;
-          const float k = qk * page_scale[sc][0][pg], e = page_scale[sc][1][pg];
-          if (!edge) {
+      for (int h = 0; h < 4; ++h) {
+        const int pg = (half * 64 + 16 * h) >> c.log_page;
+        const float k = qk * page_scale[sc][0][pg], e = page_scale[sc][1][pg];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, fmaf(s[16 * h + j], k, e));
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, visible(base + cc + 16 * h + j) ? fmaf(s[16 * h + j], k, e) : -CUDART_INF_F);
-          }
+        for (int j = 16 * h; j < 16 * h + 16; j += 2) {
+          const float2 v = fma2(make_float2(s[j], s[j + 1]), make_float2(k, k), make_float2(e, e));
+          s[j] = v.x;
+          s[j + 1] = v.y;
         }
       }
+      if (base < in_lo || base + 64 > in_hi) {
+#pragma unroll
+        for (int j = 0; j < 64; ++j) s[j] = base + j < see.z && (base + j >= see.y || base + j < see.x) ? s[j] : -CUDART_INF_F;
+      }
+#pragma unroll
+      for (int j = 0; j < 64; j += 2) top = fmaxf(fmaxf(top, s[j]), s[j + 1]);
+      half_s[half][row] = top;
+      if (cta_sync_or(pair_bar, 64, !ok)) { alive = false; ok = false; break; }
+      top = fmaxf(top, half_s[half ^ 1][row]);
       // the products of the tiles before are complete: scores of this one were issued behind them
       const bool move = top > ref + 8.f || ref == -CUDART_INF_F;
       if (__any_sync(0xFFFFFFFFu, move)) {
@@ -359,7 +375,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
         l *= by;
         if (i > 0) {
 #pragma unroll 1
-          for (int cc = 0; cc < DIM; cc += 16) {
+          for (int cc = 0; cc < DIM / 2; cc += 16) {
             float o[16];
             ctmem_ld16(t_o + cc, o);
             ctmem_wait_ld();
@@ -370,63 +386,50 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
           }
         }
       }
-      const float m = ref == -CUDART_INF_F ? 0.f : ref;
-#pragma unroll 1
-      for (int cc = 0; cc < CTILE; cc += 32) {
-        float s[32];
-        ctmem_ld32(t_s + cc, s);
-        ctmem_wait_ld();
-        uint32_t w[16];
+      const float m = ref == -CUDART_INF_F ? 0.f : -ref;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int pg = (cc + 16 * h) >> c.log_page;
-          const float k = qk * page_scale[sc][0][pg], e = page_scale[sc][1][pg] - m;
-          if (!edge) {
+      for (int h = 0; h < 4; ++h) {
+        const int pg = (half * 64 + 16 * h) >> c.log_page;
+        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[16 * h + j] = ex2(fmaf(s[16 * h + j], k, e));
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[16 * h + j] = visible(base + cc + 16 * h + j) ? ex2(fmaf(s[16 * h + j], k, e)) : 0.f;
-          }
-          float a0 = 0.f, a1 = 0.f;
-#pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            a0 += s[16 * h + j];
-            a1 += s[16 * h + j + 1];
-            w[8 * h + j / 2] = to_f16x2(s[16 * h + j], s[16 * h + j + 1]);
-          }
-          l = fmaf(a0 + a1, base + cc + 16 * h < len ? page_scale[sc][2][pg] : 0.f, l);
+        for (int j = 16 * h; j < 16 * h + 16; j += 2) {
+          float2 v = add2(make_float2(s[j], s[j + 1]), make_float2(m, m));
+          v = make_float2(ex2(v.x), ex2(v.y));
+          sum = add2(sum, v);
+          s[j / 2] = __uint_as_float(to_f16x2(v.x, v.y));
         }
-        ctmem_st16(t_s + cc / 2, w);                   // (columns whose scores have been read)
+        l = fmaf(sum.x + sum.y, base + 16 * h < len ? page_scale[sc][2][pg] : 0.f, l);
       }
+      ctmem_st32(t_s + half * 32, s);                  // (in the place of scores that both warps have read)
       ctmem_wait_st();
       ctc_fence_before();
       __syncwarp();
       if (lane == 0) { mbar_arrive(&p_bar[t]); mbar_arrive(&sc_empty[sc]); }
     }
     if (work && ok && my_nt > 0) wait(&o_bar[t], 0);
-    if (work && ok && x < packed) {
-      const uint32_t i = x / group, g = x - i * group;
-      const long long at = (long long)(r.x + (int)i) * heads + head * group + g;
-      if (lse != nullptr) lse[at] = l > 0.f || l != l ? (ref + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;
-    }
-    if (work && ok) {
-      ctc_fence_after();
+    half_s[half][row] = l;
+    if (!cta_sync_or(pair_bar, 64, !ok) && work) {
+      l += half_s[half ^ 1][row];
       const bool some = l > 0.f || l != l;
       const float inv = some ? 1.0f / l : 0.f;
       const uint32_t i = x / group, g = x - i * group;
-      __nv_bfloat16* o_at = out + ((long long)(r.x + (int)i) * heads + head * group + g) * DIM;
-#pragma unroll 1
-      for (int cc = 0; cc < DIM; cc += 16) {
-        float o[16];
-        ctmem_ld16(t_o + cc, o);
+      const long long at = (long long)(r.x + (int)i) * heads + head * group + g;
+      if (x < packed && half == 0 && lse != nullptr) lse[at] = some ? (ref + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;
+      ctc_fence_after();
+      __nv_bfloat16* o_at = out + at * DIM + half * (DIM / 2);
+#pragma unroll
+      for (int cc = 0; cc < DIM / 2; cc += 32) {
+        float o[32];
+        ctmem_ld32(t_o + cc, o);
         ctmem_wait_ld();
         if (x < packed) {
-          uint32_t w[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(some ? o[2 * j] * inv : 0.f, some ? o[2 * j + 1] * inv : 0.f);
-          *reinterpret_cast<uint4*>(o_at + cc) = make_uint4(w[0], w[1], w[2], w[3]);
-          *reinterpret_cast<uint4*>(o_at + cc + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+          for (int j = 0; j < 32; j += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = some ? pack_bf16x2(o[j + 2 * e] * inv, o[j + 2 * e + 1] * inv) : 0u;
+            *reinterpret_cast<uint4*>(o_at + cc + j) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
         }
       }
     }
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   }
   ctc_fence_before();
   __syncthreads();
-  if (warp == 13) tmem_free(tmem, 512);
+  if (warp == 19) tmem_free(tmem, 512);
 }
 
 }  // namespace ficoco
