@@ -77,6 +77,12 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(smem_u32(bar)) : "memory");
 }
 
+// bulk_load to an address in shared memory.
+__device__ __forceinline__ void bulk_load_at(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
 // A pair of values as NT e4m3 terms each: codes[t] holds both values' term t, the first one's in the low byte.  Term t is
 // 16^t times what it stands for; with UP false the terms stand for themselves, so that products with all of them can share an
 // accumulator (the smallest step of e4m3, 2^-9, then bounds all of them).

@@ -80,6 +80,7 @@ struct PromptPlan {
   static constexpr int V16 = 2 * CODES;
   static constexpr int K_ST = 3, V_ST = 2, V16_ST = 2, SC_ST = 4;
   static constexpr int SMEM = 1024 + 2 * Q_TILE + K_ST * CODES + V_ST * CODES + V16_ST * V16;
+  static_assert(PROMPT_ROWS * DIM * 2 <= V16_ST * V16, "the query rows' place");
   static_assert(SMEM + 4096 <= 227 * 1024, "one CTA per SM");
 };
 
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   constexpr int K_ST = PL::K_ST, V_ST = PL::V_ST, V16_ST = PL::V16_ST, SC_ST = PL::SC_ST;
   extern __shared__ unsigned char prompt_raw[];
   __shared__ uint64_t k_full[K_ST], k_empty[K_ST], v_full[V_ST], v_empty[V_ST], w_full[V16_ST], w_empty[V16_ST];
-  __shared__ uint64_t sc_full[SC_ST], sc_empty[SC_ST], q_bar, s_bar[2], p_bar[2], o_bar[2], drain_bar;
+  __shared__ uint64_t sc_full[SC_ST], sc_empty[SC_ST], raw_bar, q_bar, s_bar[2], p_bar[2], o_bar[2], drain_bar;
   __shared__ uint32_t tmem_s;
   __shared__ int dead_s;
   __shared__ float page_scale[SC_ST][3][8];            // key scale, log2 of the value scale, 1 / value scale
@@ -110,6 +111,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     for (int s = 0; s < V16_ST; ++s) { mbar_init(&w_full[s], 2); mbar_init(&w_empty[s], 1); }
     for (int s = 0; s < SC_ST; ++s) { mbar_init(&sc_full[s], 1); mbar_init(&sc_empty[s], 16); }
     for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 8); mbar_init(&o_bar[s], 1); }
+    mbar_init(&raw_bar, PROMPT_ROWS);
     mbar_init(&q_bar, 16);
     mbar_init(&drain_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -256,6 +258,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     // ---------------- values: e4m3 -> fp16, thread = 16 dimensions of every (64 * 16 / DIM)-th token ---------------------
     constexpr int CHUNKS = DIM / 16;
     const int ct = tid - 512, ch = ct % CHUNKS;
+    if (n_tiles > 0) wait(&q_bar, 0);                  // (the query rows lie where the values go)
     for (int i = 0; ok && i < n_tiles; ++i) {
       wait(&v_full[i % V_ST], i / V_ST);
       if (i >= V16_ST) wait(&w_empty[i % V16_ST], i / V16_ST - 1);
@@ -285,34 +288,40 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     // ---------------- softmax: thread = row and half of the tokens ---------------------------------------------------------
     const int t = warp >> 3, half = warp >> 2 & 1, wr = warp & 3, row = t * 128 + wr * 32 + lane, pair_bar = 1 + t * 4 + wr;
     if (work) {
-      // the query rows of the CTA, all loads in flight at once
-      constexpr int LANES = DIM / 8, AT_ONCE = 512 / LANES, N_AT = PROMPT_ROWS / AT_ONCE;
+      // The query rows of the CTA come by bulk copies to where converted values will lie, and are split in a rolled loop: 1200
+      // instructions in a line, run once, took 14000 cycles, most of them to fetch the instructions.
+      const uint32_t raw = w_ring;
+      if (tid < PROMPT_ROWS) {
+        const uint32_t x = x0 + tid, i = x / group, g = x - i * group;
+        if (x < packed) {
+          mbar_expect_tx(&raw_bar, DIM * 2);
+          bulk_load_at(raw + tid * (DIM * 2), q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM, DIM * 2, &raw_bar);
+        } else {
+          mbar_arrive(&raw_bar);
+        }
+      }
+      wait(&raw_bar, 0);
+      constexpr int LANES = DIM / 8, AT_ONCE = 512 / LANES;
       const int chunk = tid % LANES;
-      Raw8<__nv_bfloat16> raw[N_AT];
-      float scale[N_AT];
+#pragma unroll 1
+      for (int x = tid / LANES; x < PROMPT_ROWS; x += 2 * AT_ONCE) {
+        float f[2][8], scale[2];
 #pragma unroll
-      for (int p = 0; p < N_AT; ++p) {
-        const uint32_t x = x0 + p * AT_ONCE + tid / LANES;
-        const uint32_t i = x / group, g = x - i * group;
-        if (x < packed) raw[p].load(q + (long long)(r.x + (int)i) * q_stride + (long long)(head * group + g) * DIM + chunk * 8);
-        else raw[p].clear();
-      }
+        for (int p = 0; p < 2; ++p) {
+          uint4 u4 = make_uint4(0u, 0u, 0u, 0u);
+          if (x0 + x + p * AT_ONCE < packed)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u4.x), "=r"(u4.y), "=r"(u4.z), "=r"(u4.w)
+                         : "r"(raw + (x + p * AT_ONCE) * (DIM * 2) + chunk * 16) : "memory");
+          unpack(u4, f[p], q);
+        }
 #pragma unroll
-      for (int p = 0; p < N_AT; ++p) {
-        float f[8];
-        raw[p].get(f);
-        scale[p] = query_scale<DIM>(f);
-      }
+        for (int p = 0; p < 2; ++p) scale[p] = query_scale<DIM>(f[p]);
 #pragma unroll
-      for (int p = 0; p < N_AT; ++p) {
-        const int x = p * AT_ONCE + tid / LANES;
-        float f[8];
-        raw[p].get(f);
-        store_query<DIM, 2, false>(f, scale[p], q_base + (x >> 7) * PL::Q_TILE, x & 127, 128, chunk);
-      }
-      if (chunk == 0) {
-#pragma unroll
-        for (int p = 0; p < N_AT; ++p) q_scale[p * AT_ONCE + tid / LANES] = scale[p] * scale_log2;
+        for (int p = 0; p < 2; ++p) {
+          const int row_x = x + p * AT_ONCE;
+          store_query<DIM, 2, false>(f[p], scale[p], q_base + (row_x >> 7) * PL::Q_TILE, row_x & 127, 128, chunk);
+          if (chunk == 0) q_scale[row_x] = scale[p] * scale_log2;
+        }
       }
       fence_proxy_async();
       __syncwarp();
