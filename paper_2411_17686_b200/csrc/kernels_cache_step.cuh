@@ -196,6 +196,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     int nt_most = 0;
     StepSeq s0;
     long long size = 0;
+#pragma unroll 1
     for (int b0 = 0; b0 < c.batch; b0 += 32) {
       size = 0;
       if (b0 + lane < c.batch) {
@@ -218,6 +219,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     walk.b = 0; walk.head = walk.block = walk.tile = 0;
     if (walk.left > 0) {
       long long before = 0;
+#pragma unroll 1
       for (int b0 = 0;; b0 += 32) {
         if (c.batch > 32) {                                    // (the last 32 sequences' sizes are at hand)
           size = 0;
@@ -272,6 +274,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       x.page = -1;
       x.ks = x.vs = 1.f;
       int b = 0, base = 0, len = 0;
+#pragma unroll 1
       for (x.tiles = 0; x.tiles < most; ++x.tiles, ++t_next) {
         if (t_next >= t_end) {
           if (!step_next(walk, g, c, cu, rows, group, RB, mask, status)) break;
@@ -311,8 +314,10 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       if (lane == 0) mbar_arrive(&scale_bar[st_before]);
     };
     bool first = true;
+#pragma unroll 1
     while (ok && now.tiles > 0) {
       if (!first) { fetch_scales(soon); assign(later, batch_tiles); }
+#pragma unroll 1
       for (int t = 0; t < now.tiles; ++t, ++i) {
         const bool mine_now = lane >> log_ppt == t && now.page >= 0;
         const uint32_t load = bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine_now));
@@ -349,6 +354,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     if (!ok) {
       if (lane == 0) atomicOr(status, STATUS_TIMEOUT);
       // no copy outlives the CTA: the tiles asked for last
+#pragma unroll 1
       for (int k = max(0, i - NST); k < i; ++k) {
         mbar_wait(&k_full[k % NST], (k / NST) & 1, wait_ns);
         mbar_wait(&v_full[k % NST], (k / NST) & 1, wait_ns);
@@ -360,6 +366,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     constexpr uint32_t id_s = cache_idesc(128, N, 0, 0), id_o = cache_idesc(DIM, N, 1, 0);
     StepSeg g;
     int seg = -1, left = 0, st = 0, wrap = 0, st_prev = 0, wrap_prev = 0;
+#pragma unroll 1
     for (int i = 0;; ++i) {
       bool more = true;
       if (left == 0) {
@@ -414,6 +421,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     StepSeg g;
     int i = 0, st = 0, wrap = 0;
     const int pg = tid >> c.log_page;
+#pragma unroll 1
     for (int seg = 0; ok && step_next(walk, g, c, cu, rows, group, RB, mask, status); ++seg) {
       const int buf_q = seg & 1;
       wait(&q_bar[buf_q], seg >> 1);                           // the rows' scales and masks
@@ -425,6 +433,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       const int i_last = min((int)(((uint32_t)g.block * RB + RB - 1) / (uint32_t)group), g.s.n_rows - 1);
       const int in_hi = seen(mask, g.s.len - g.s.n_rows + i_first, g.s.len).z;
       const int in_lo = seen(mask, g.s.len - g.s.n_rows + i_last, g.s.len).y;
+#pragma unroll 1
       for (int t = g.tile; t < g.tile + g.count; ++t, ++i) {
         const int base = step_token0(g.s, t), buf = i & 1;
         wait(&scale_bar[st], wrap);
@@ -544,14 +553,23 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     };
     long long at = piece0;                                     // where this item's tiles start in the list
     int n_seg = 0;                                             // items described so far
-    for (; n_seg < 3 && ahead(n_seg); ++n_seg) {
-      cta_sync(2, 128);
-      if (n_seg < 2) put_q(seg_s[n_seg], n_seg);
-    }
-    bool more = n_seg == 3;
+    bool more = true;
     int i = 0;
     constexpr int PER = RB / 8;                                // maxima per lane: lane = (softmax warp, row % 8)
-    for (int seg = 0; seg < n_seg; ++seg) {
+    // Three turns ahead of item 0 only fetch and place queries: the code stands here once (all of a kernel's roles share the
+    // instruction caches, and what is fetched for the first time takes longer than what it does).
+#pragma unroll 1
+    for (int seg = -3; seg < n_seg; ++seg) {
+      if (seg < 0) {
+        cta_sync(2, 128);                                      // the items' descriptions
+        if (seg + 2 >= 0 && seg + 2 < n_seg) put_q(seg_s[seg + 2], seg & 1);
+        if (more) {
+          more = ahead(n_seg);
+          n_seg += more;
+        }
+        if (n_seg == 0) break;
+        continue;
+      }
       const int buf_q = seg & 1;
       const StepSeg& g = seg_s[seg & 3];
       const int count = g.count;
@@ -560,6 +578,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       for (int r = 0; r < RB; ++r) acc[r] = 0.f;
 #pragma unroll
       for (int p = 0; p < PER; ++p) m_run[p] = -CUDART_INF_F;
+#pragma unroll 1
       for (int t = 1; t <= count; ++t, ++i) {
         const int buf = i & 1;
         wait(&p_bar[buf], i >> 1);                             // the maxima
