@@ -242,8 +242,10 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   ctx_set_launches(ctx, 0);
   if (a->rows == 0) return FICOCO_OK;
   const float scale_log2 = a->scale * 1.4426950408889634f;
-  if (c.dim == 128) return attend_dim<128>(ctx, x, c, a, scale_log2, st);
-  if (c.dim == 64) return attend_dim<64>(ctx, x, c, a, scale_log2, st);
+  // (the tensor-core kernels count tiles of 8 rows by 128 tokens in 32 bits; what could exceed that takes the kernel without tiles)
+  const double most_tiles = ((double)a->rows * (a->heads / c.kv) / 8 + c.batch) * c.kv * ((double)c.max_pages * c.page / CTILE + 2);
+  if (c.dim == 128 && most_tiles < 2e9) return attend_dim<128>(ctx, x, c, a, scale_log2, st);
+  if (c.dim == 64 && most_tiles < 2e9) return attend_dim<64>(ctx, x, c, a, scale_log2, st);
   const dim3 grid(a->rows, a->heads);
   ctx_prof_tick(ctx, st, "k_cache_attention_simt");
   if (a->dtype == FICOCO_BF16)

@@ -54,7 +54,7 @@ struct StepSeg {
   StepSeq s;
 };
 struct StepWalk {
-  long long left;                          // tiles of the piece that are still to come
+  int left;                                // tiles of the piece that are still to come
   int b, head, block, tile;
   StepSeq s;
 };
@@ -70,15 +70,21 @@ __device__ __forceinline__ bool step_next(StepWalk& w, StepSeg& g, const CacheVi
     w.s = step_seq(c, cu, rows, group, rb, mask, ++w.b, status);
   }
   g.b = w.b; g.head = w.head; g.block = w.block; g.tile = w.tile; g.s = w.s;
-  g.count = (int)min((long long)(w.s.nt - w.tile), w.left);
+  g.count = min(w.s.nt - w.tile, w.left);
   w.tile += g.count;
   w.left -= g.count;
   return true;
 }
-// x * y / z for y, z < 512; in 32 bits where the product fits (a 64-bit division is some 100 instructions)
-__device__ __forceinline__ long long mul_div(long long x, int y, int z) {
-  return x < (1 << 23) ? (long long)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
-}
+// The list of `total` tiles (below 2^31: the host sees to that) in n pieces, the first `more` of them a tile longer.
+struct StepCut {
+  int base, more;
+  __device__ __forceinline__ StepCut(int total, int n) : base(total / n), more(total - total / n * n) {}
+  __device__ __forceinline__ int start(int k) const { return k * base + min(k, more); }
+  __device__ __forceinline__ int piece_of(int x) const {       // base > 0
+    const int edge = more * (base + 1);
+    return x < edge ? x / (base + 1) : more + (x - edge) / base;
+  }
+};
 __device__ __forceinline__ int step_token0(const StepSeq& s, int tile) {      // first token of a tile of the item
   return (tile < s.t_sink ? tile : tile - s.t_sink + s.t0) * CTILE;
 }
@@ -190,48 +196,45 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
   if (tid == 0) dead_s = (*reinterpret_cast<const volatile unsigned*>(status) & STATUS_TIMEOUT) ? 1 : 0;
   // ---- this CTA's piece of the list.  Every warp finds it by itself (lane = sequence), so that no barrier is waited for ------
   StepWalk walk;
-  long long piece0, piece1, total = 0;
-  int n_cta;
+  int total = 0, n_cta, piece0;
   {
-    int nt_most = 0;
+    int nt_most = 0, size = 0;
     StepSeq s0;
-    long long size = 0;
 #pragma unroll 1
     for (int b0 = 0; b0 < c.batch; b0 += 32) {
       size = 0;
       if (b0 + lane < c.batch) {
         s0 = step_seq(c, cu, rows, group, RB, mask, b0 + lane, status);
-        size = (long long)s0.blocks * c.kv * s0.nt;
+        size = s0.blocks * c.kv * s0.nt;
         if (size > 0) nt_most = max(nt_most, s0.nt);
       }
       total += size;
     }
-#pragma unroll 1
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    total = __reduce_add_sync(0xFFFFFFFFu, total);
     nt_most = __reduce_max_sync(0xFFFFFFFFu, nt_most);
     // CTAs that get a piece: no more than tiles, nor so many that the longest item would be cut into more than STEP_MAX_PARTS
-    n_cta = (int)min((long long)gridDim.x, total);
-    if ((long long)n_cta * nt_most > (STEP_MAX_PARTS - 1) * total) n_cta = (int)max(1ll, (STEP_MAX_PARTS - 1) * total / nt_most);
-    const bool has_piece = (int)blockIdx.x < n_cta;
-    piece0 = has_piece ? mul_div(total, blockIdx.x, n_cta) : 0;
-    piece1 = has_piece ? mul_div(total, blockIdx.x + 1, n_cta) : 0;
-    walk.left = piece1 - piece0;
+    n_cta = max(1, min((int)gridDim.x, total));
+    const float most = (float)(STEP_MAX_PARTS - 2) * (float)total;
+    if ((float)n_cta * (float)nt_most > most) n_cta = max(1, (int)(most / (float)nt_most));
+    const StepCut cut(total, n_cta);
+    piece0 = cut.start(blockIdx.x);
+    walk.left = (int)blockIdx.x < n_cta ? cut.start(blockIdx.x + 1) - piece0 : 0;
     walk.b = 0; walk.head = walk.block = walk.tile = 0;
     if (walk.left > 0) {
-      long long before = 0;
+      int before = 0;
 #pragma unroll 1
       for (int b0 = 0;; b0 += 32) {
         if (c.batch > 32) {                                    // (the last 32 sequences' sizes are at hand)
           size = 0;
           if (b0 + lane < c.batch) {
             s0 = step_seq(c, cu, rows, group, RB, mask, b0 + lane, status);
-            size = (long long)s0.blocks * c.kv * s0.nt;
+            size = s0.blocks * c.kv * s0.nt;
           }
         }
-        long long upto = size;
-#pragma unroll 1
+        int upto = size;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+          const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
           upto += lane >= o ? v : 0;
         }
         const unsigned reached = __ballot_sync(0xFFFFFFFFu, before + upto > piece0);
@@ -245,11 +248,11 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         walk.s.n_rows = __shfl_sync(0xFFFFFFFFu, s0.n_rows, l); walk.s.blocks = __shfl_sync(0xFFFFFFFFu, s0.blocks, l);
         walk.s.t_sink = __shfl_sync(0xFFFFFFFFu, s0.t_sink, l); walk.s.t0 = __shfl_sync(0xFFFFFFFFu, s0.t0, l);
         walk.s.nt = __shfl_sync(0xFFFFFFFFu, s0.nt, l);
-        const long long off = piece0 - before - __shfl_sync(0xFFFFFFFFu, upto - size, l);
-        const int item = (int)(off < (1ll << 32) ? (long long)((uint32_t)off / (uint32_t)walk.s.nt) : off / walk.s.nt);
-        walk.tile = (int)(off - (long long)item * walk.s.nt);
-        walk.block = (int)((uint32_t)item / (uint32_t)c.kv);
-        walk.head = item - walk.block * c.kv;
+        const uint32_t off = (uint32_t)(piece0 - before - __shfl_sync(0xFFFFFFFFu, upto - size, l));
+        const uint32_t item = off / (uint32_t)walk.s.nt;
+        walk.tile = (int)(off - item * (uint32_t)walk.s.nt);
+        walk.block = (int)(item / (uint32_t)c.kv);
+        walk.head = (int)item - walk.block * c.kv;
         break;
       }
     }
@@ -551,7 +554,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       if (bt == 0) seg_s[k & 3] = g;
       return true;
     };
-    long long at = piece0;                                     // where this item's tiles start in the list
+    int at = piece0;                                           // where this item's tiles start in the list
     int n_seg = 0;                                             // items described so far
     bool more = true;
     int i = 0;
@@ -656,20 +659,13 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         }
       } else {
         // A cut item.  Its first piece is the last one of CTA `owner`, the others are the first ones of the CTAs behind it.
-        const long long item0 = at - g.tile, item1 = item0 + g.s.nt;
         float* mine_p = partials + ((size_t)blockIdx.x * 2 + (g.tile == 0 ? 1 : 0)) * PL::PART;
 #pragma unroll 1
         for (int u = bt; u < nr * (DIM / 4); u += 128)
           __stcg(reinterpret_cast<float4*>(mine_p + u * 4), *reinterpret_cast<const float4*>(&out_s[0][0] + u * 4));
         if (bt < nr) { __stcg(mine_p + RB * DIM + bt, top_s[bt]); __stcg(mine_p + RB * DIM + RB + bt, den_s[bt]); }
-        auto cta_of = [&](long long x) {
-          int k = (int)((float)(x + 1) * (float)n_cta / (float)total);
-          k = min(max(k, 0), n_cta - 1);
-          while (mul_div(total, k, n_cta) > x) --k;
-          while (mul_div(total, k + 1, n_cta) <= x) ++k;
-          return k;
-        };
-        const int owner = cta_of(item0), parts = cta_of(item1 - 1) - owner + 1;
+        const StepCut cut(total, n_cta);
+        const int owner = cut.piece_of(at - g.tile), parts = cut.piece_of(at - g.tile + g.s.nt - 1) - owner + 1;
         cta_sync(2, 128);
         if (bt == 0) last_s = atom_acq_rel_add(&counters[owner], 1) == parts - 1;
         cta_sync(2, 128);
