@@ -65,8 +65,8 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
   uint8_t* dst = (is_v ? c.v : c.k) + (at << c.log_page) * c.dim;
   float* scale = (is_v ? c.vs : c.ks) + at;
   const float old = s0 > 0 ? *scale : 0.f;
-  const int dim_log = 31 - __clz(vecs), row_of_pow2 = (vecs & (vecs - 1)) == 0;    // (a division per vector otherwise)
-  auto row_of = [&](int i) { return row_of_pow2 ? i >> dim_log : i / vecs; };
+  const uint32_t inv_vecs = ((1u << 20) + vecs - 1) / vecs;     // i / vecs as a product: exact for i < 2^20 / vecs, a page has 2^12
+  auto row_of = [&](int i) { return (int)((uint32_t)i * inv_vecs >> 20); };
   auto from_row = [&](int i, int row) { return src + row * stride + (i - row * vecs) * 8; };
 
   Raw8<T> held[HELD];
@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
   };
 #pragma unroll
   for (int x = 0; x < HELD; ++x) look(held[x], lane + (x << log_team));
+#pragma unroll 1
   for (int i = lane + (HELD << log_team); i < total; i += team) {
     Raw8<T> raw;
     raw.load(from_row(i, row_of(i)));
@@ -102,6 +103,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
   auto is_bad = [&](int row) { return (poisoned[mine >> 1][row >> 5] >> (row & 31) & 1u) != 0; };
   if (any_bad) {                          // rare: once more without the rows that do not count
     top = 0;
+#pragma unroll 1
     for (int i = lane; i < total; i += team) {
       const int row = row_of(i);
       if (is_bad(row)) continue;
@@ -116,6 +118,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
   const float s = fmaxf(scale_of(amax), old), inv = 1.0f / s;
   if (s0 > 0 && s > old) {                // the older codes of the page move to the larger scale
     const float f = old * inv;
+#pragma unroll 1
     for (int i = lane; i < s0 * vecs; i += team) {
       uint2* p = reinterpret_cast<uint2*>(dst) + i;
       float x[8];
@@ -140,6 +143,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
     const int i = lane + (x << log_team);
     if (i < total) put(held[x], i);
   }
+#pragma unroll 1
   for (int i = lane + (HELD << log_team); i < total; i += team) {
     Raw8<T> raw;
     raw.load(from_row(i, row_of(i)));
@@ -190,9 +194,9 @@ __global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheVi
   const int vecs = c.dim >> 4, total = on ? s1 * vecs : 0;      // vectors of 16 codes
   const uint8_t* src = is_v ? c.v : c.k;
   const float* scales = is_v ? c.vs : c.ks;
-  const int dim_log = 31 - __clz(vecs), row_of_pow2 = (vecs & (vecs - 1)) == 0;
+  const uint32_t inv_vecs = ((1u << 20) + vecs - 1) / vecs;     // i / vecs as a product: exact for i < 2^20 / vecs, a page has 2^11
   auto fetch = [&](int i, uint4& codes, float& s) {
-    const int row = row_of_pow2 ? i >> dim_log : i / vecs;
+    const int row = (int)((uint32_t)i * inv_vecs >> 20);
     const int2 f = row_from[row];
     const size_t at = (size_t)max(f.x, 0) * c.kv + head;
     codes = *reinterpret_cast<const uint4*>(src + ((at << c.log_page) + f.y) * c.dim + (i - row * vecs) * 16);
@@ -220,6 +224,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheVi
   float amax = 0.f;
 #pragma unroll
   for (int x = 0; x < COMPACT_HELD; ++x) amax = fmaxf(amax, look(held[x], hs[x]));
+#pragma unroll 1
   for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
     uint4 u4;
     float s;
@@ -246,6 +251,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheVi
     const int i = lane + (x << log_team);
     if (i < total) put(i, held[x], hs[x]);
   }
+#pragma unroll 1
   for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
     uint4 u4;
     float by;

@@ -677,28 +677,30 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
             const int r = u / (DIM / 4), d4 = (u % (DIM / 4)) * 4;
             float top = -CUDART_INF_F, den = 0.f;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-            // four parts at a time, in order, the sums brought to the larger maximum
+            // eight parts at a time, in order, the sums brought to the larger maximum
 #pragma unroll 1
-            for (int k0 = 0; k0 < parts; k0 += 4) {
-              float m4[4], l4[4];
-              float4 v4[4];
+            for (int k0 = 0; k0 < parts; k0 += 8) {
+              float m8[8], l8[8];
+              float4 v8[8];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
+              for (int k = 0; k < 8; ++k) {
                 const float* pk = part(min(k0 + k, parts - 1));
-                m4[k] = k0 + k < parts ? __ldcg(pk + RB * DIM + r) : -CUDART_INF_F;
-                l4[k] = __ldcg(pk + RB * DIM + RB + r);
-                v4[k] = __ldcg(reinterpret_cast<const float4*>(pk + r * DIM + d4));
+                m8[k] = __ldcg(pk + RB * DIM + r);
+                l8[k] = __ldcg(pk + RB * DIM + RB + r);
+                v8[k] = __ldcg(reinterpret_cast<const float4*>(pk + r * DIM + d4));
               }
-              const float mn = fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), top), ref = mn == -CUDART_INF_F ? 0.f : mn;
-              const float w0 = ex2(top - ref);
+              float mn = top;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) mn = fmaxf(mn, m8[k]);       // (the last part again in the places behind it)
+              const float ref = mn == -CUDART_INF_F ? 0.f : mn, w0 = ex2(top - ref);
               top = mn;
               den *= w0; a.x *= w0; a.y *= w0; a.z *= w0; a.w *= w0;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
+              for (int k = 0; k < 8; ++k) {
                 if (k0 + k >= parts) break;
-                const float w = ex2(m4[k] - ref);
-                den = fmaf(w, l4[k], den);
-                a.x = fmaf(w, v4[k].x, a.x); a.y = fmaf(w, v4[k].y, a.y); a.z = fmaf(w, v4[k].z, a.z); a.w = fmaf(w, v4[k].w, a.w);
+                const float w = ex2(m8[k] - ref);
+                den = fmaf(w, l8[k], den);
+                a.x = fmaf(w, v8[k].x, a.x); a.y = fmaf(w, v8[k].y, a.y); a.z = fmaf(w, v8[k].z, a.z); a.w = fmaf(w, v8[k].w, a.w);
               }
             }
             finish(r, d4, a, top, den);
