@@ -73,6 +73,12 @@ __device__ __forceinline__ uint32_t f16x2_of(uint32_t codes) {
   return h;
 }
 
+// The bits [lo, hi) of a word, for any lo and hi.
+__device__ __forceinline__ uint32_t bits(int lo, int hi) {
+  const uint32_t below_hi = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u;
+  return lo <= 0 ? below_hi : lo >= 32 ? 0u : below_hi & ~((1u << lo) - 1u);
+}
+
 template <int DIM>
 struct PromptPlan {
   static constexpr int Q_TERM = 128 * DIM, Q_TILE = 2 * Q_TERM;      // two e4m3 terms of a row tile
@@ -367,8 +373,14 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
         }
       }
       if (base < in_lo || base + 64 > in_hi) {
+        // a bit per token that the row sees (comparing 64 token indexes with the row's bounds cost a tenth of the kernel, in registers
+        // of the tiles that need none of it)
 #pragma unroll
-        for (int j = 0; j < 64; ++j) s[j] = base + j < see.z && (base + j >= see.y || base + j < see.x) ? s[j] : -CUDART_INF_F;
+        for (int w = 0; w < 2; ++w) {
+          const uint32_t on = bits(see.y - base - 32 * w, see.z - base - 32 * w) | bits(0, see.x - base - 32 * w);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[32 * w + j] = on & 1u << j ? s[32 * w + j] : -CUDART_INF_F;
+        }
       }
 #pragma unroll
       for (int j = 0; j < 64; j += 2) top = fmaxf(fmaxf(top, s[j]), s[j + 1]);
