@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   ctc_fence_after();
   grid_dep_launch();       // behind the barrier: a dependent that took this SM's TMEM first would wait for it for ever
   const uint32_t tmem = tmem_s;
-  const bool work = pair >= 0 && u >= unit0(b) && !dead_s;
+  const bool work = pair >= 0 && u >= unit0(b) && !dead_s && tmem == 0;
   // ---- tiles of tokens that the rows see ----------------------------------------------------------------------------
   const uint32_t x0 = (uint32_t)max(pair, 0) * PROMPT_ROWS;
   auto query = [&](uint32_t x) { return (int)(min(x, packed - 1) / group); };      // of packed row x
@@ -203,7 +203,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     }
   } else if (warp == 19) {
     // ---------------- MMA: per tile of tokens, each row tile's weights times values, then its next scores ------------------
-    const uint32_t u_tmem = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    // (all 512 columns are this CTA's, so its addresses start at 0: as a constant they stay in uniform registers)
+    constexpr uint32_t u_tmem = 0;
     constexpr uint32_t id_s = cache_idesc(128, CTILE, 0, 0), id_o = cache_idesc(128, DIM, 0, 1);
     auto scores = [&](int t, int i) {
       const uint32_t qa = q_base + t * PL::Q_TILE;
@@ -271,19 +272,27 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
       if (!ok) break;
       const uint32_t v = v_ring + (i % V_ST) * PL::CODES, w = w_ring + (i % V16_ST) * PL::V16 + (ch >> 2) * (CTILE * 128);
       const int left = len - token0(i);                // tokens behind it: whatever the slot holds must not meet a weight of 0
-#pragma unroll 4
-      for (int j = ct / CHUNKS; j < CTILE; j += 64 / CHUNKS) {
-        uint32_t a[4];
-        const int sw = DIM == 128 ? ch ^ (j & 7) : ch ^ ((j >> 1) & 3);
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
-                     : "r"(v + j * DIM + sw * 16) : "memory");
-        const bool on = j < left;
+      constexpr int STEP = 64 / CHUNKS;
+#pragma unroll 1
+      for (int j0 = ct / CHUNKS; j0 < CTILE; j0 += 4 * STEP) {
+        uint32_t a[4][4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) a[x] = on ? a[x] : 0u;
-        const uint32_t to = w + j * 128;
-        const int c2 = (ch & 3) * 2;                   // two 16-byte pieces of the token's 128-byte row
-        st_shared16(to + ((c2 ^ (j & 7)) << 4), f16x2_of(a[0]), f16x2_of(a[0] >> 16), f16x2_of(a[1]), f16x2_of(a[1] >> 16));
-        st_shared16(to + (((c2 + 1) ^ (j & 7)) << 4), f16x2_of(a[2]), f16x2_of(a[2] >> 16), f16x2_of(a[3]), f16x2_of(a[3] >> 16));
+        for (int e = 0; e < 4; ++e) {                  // (four loads in flight: one at a time, a tile took 2800 cycles)
+          const int j = j0 + e * STEP, sw = DIM == 128 ? ch ^ (j & 7) : ch ^ ((j >> 1) & 3);
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a[e][0]), "=r"(a[e][1]), "=r"(a[e][2]), "=r"(a[e][3])
+                       : "r"(v + j * DIM + sw * 16) : "memory");
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = j0 + e * STEP;
+          const bool on = j < left;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) a[e][x] = on ? a[e][x] : 0u;
+          const uint32_t to = w + j * 128;
+          const int c2 = (ch & 3) * 2;                 // two 16-byte pieces of the token's 128-byte row
+          st_shared16(to + ((c2 ^ (j & 7)) << 4), f16x2_of(a[e][0]), f16x2_of(a[e][0] >> 16), f16x2_of(a[e][1]), f16x2_of(a[e][1] >> 16));
+          st_shared16(to + (((c2 + 1) ^ (j & 7)) << 4), f16x2_of(a[e][2]), f16x2_of(a[e][2] >> 16), f16x2_of(a[e][3]), f16x2_of(a[e][3] >> 16));
+        }
       }
       fence_proxy_async();
       __syncwarp();
