@@ -281,7 +281,8 @@ int ficoco_status(ficoco_ctx* ctx, void* cuda_stream, int* device_status);
 /* Testing hook for the bounded waits.  wait_ns > 0 sets the time after which a device-side wait
  * of this context gives up (default 20 ms); extra_arrivals > 0 makes the fused filter kernel wait
  * for that many arrivals more than will ever come, so that the wait runs out by itself (nothing
- * spins past the bound, nothing faults); 0 restores normal operation.  Affects later calls. */
+ * spins past the bound, nothing faults), and so do the tensor-core kernels of the 8-bit cache; 0 restores normal operation.
+ * Affects later calls. */
 int ficoco_debug_waits(ficoco_ctx* ctx, long long wait_ns, int extra_arrivals);
 
 /* Testing hook: waits on a shared-memory barrier that nothing completes with the context's bound

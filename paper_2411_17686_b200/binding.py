@@ -591,7 +591,8 @@ class Context:
         """Writes k, v (cuda [rows, kv_heads, head_dim], bf16 or fp32, rows may be strided) as the last tokens of the
         sequences; cu_rows: cuda int32 [batch + 1].  ``cache.lengths`` already counts them."""
         cs = cache.struct
-        if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (cs.kv_heads, cs.head_dim):
+        self._same_device(cache, k)
+        if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.shape[1:] != (cs.kv_heads, cs.head_dim):
             raise ValueError(f"k and v must both be [rows, {cs.kv_heads}, {cs.head_dim}] of one type")
         a = ficoco_append_args(k.data_ptr(), v.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1),
                                _rows3("k", k, cs.head_dim), _rows3("v", v, cs.head_dim), _dtype_code(k), k.shape[0])
@@ -599,8 +600,13 @@ class Context:
         if rc:
             _check(self.h, rc)
 
+    def _same_device(self, cache: PagedCache, t) -> None:
+        if cache.device.index != self.device or t.device != cache.device:
+            raise ValueError(f"the context is on cuda:{self.device}, the cache on {cache.device}, the rows on {t.device}")
+
     def _attention_args(self, cache, q, cu_rows, scale, causal, window, sinks) -> ficoco_attention_args:
         cs = cache.struct
+        self._same_device(cache, q)
         stride = _rows3("q", q, cs.head_dim)
         return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1), None, None, stride,
                                      cs.head_dim ** -0.5 if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
@@ -655,6 +661,7 @@ class Context:
 
     def ficoco_cache_copy(self, cache: PagedCache, src, dst, *, stream: Optional[int] = None) -> None:
         """Copies page src[i] to page dst[i] (cuda int32 tensors of one length; pairs with a negative page are skipped)."""
+        self._same_device(cache, src)
         rc = self.lib.ficoco_cache_copy(self.h, cache.struct, _int32("src", src), _int32("dst", dst, src.numel()), src.numel(),
                                         _current_stream(cache.device) if stream is None else stream)
         if rc:
@@ -666,6 +673,7 @@ class Context:
         (cuda int32 [batch, pages], other pages than the cache's).  Returns the new lengths (cuda int32 [batch])."""
         import torch
         cs = cache.struct
+        self._same_device(cache, to_table)
         if to_table.dtype != torch.int32 or to_table.dim() != 2 or to_table.shape[0] != cs.batch or not to_table.is_cuda or \
                 to_table.stride(1) != 1:
             raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")

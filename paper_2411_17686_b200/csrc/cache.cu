@@ -145,7 +145,7 @@ int attend_step(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const f
   ctx_prof_tick(ctx, st, "k_cache_step");
   CACHE_TRY(ctx, launch(k_cache_step<T, DIM, NT, RB>, dim3(x.num_sms * SCRATCH_CTAS_PER_SM), STEP_THREADS, PL::SMEM, st, km, vm, c,
                         (const T*)a->q, a->cu_rows, (T*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a),
-                        counters, partials, x.status, x.wait_ns));
+                        counters, partials, x.status, x.wait_ns, x.extra_arrivals));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;
@@ -161,7 +161,7 @@ int attend_prompt(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const
   ctx_prof_tick(ctx, st, "k_cache_prompt");
   CACHE_TRY(ctx, launch(k_cache_prompt<DIM>, dim3((unsigned)(units * c.kv)), PROMPT_THREADS, PL::SMEM, st, km, vm, c,
                         (const __nv_bfloat16*)a->q, a->cu_rows, (__nv_bfloat16*)a->out, a->lse, a->q_stride, scale_log2, a->rows, a->heads,
-                        mask_rule(a), x.status, x.wait_ns));
+                        mask_rule(a), x.status, x.wait_ns, x.extra_arrivals));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;
@@ -170,7 +170,11 @@ template <int DIM>
 int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
   if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, st);
   const long long rows = (long long)a->rows * (a->heads / c.kv);       // of all sequences, per key/value head
-  if (rows > 32ll * c.batch) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
+  // The prompt kernel takes 256 rows per CTA and needs about 5000 cycles for a tile of tokens, one CTA per SM; the step kernel takes 16
+  // rows per item, two CTAs per SM, about 3000 cycles a tile: whichever has the shorter line (the tiles per row are the same).
+  const long long prompt_ctas = std::max(1ll, rows / PROMPT_ROWS) * c.kv, step_items = (rows / 16 + 1) * c.kv;
+  const long long prompt_time = (prompt_ctas + x.num_sms - 1) / x.num_sms * 5000, step_time = step_items * 3000 / (2 * x.num_sms);
+  if (rows > 32ll * c.batch && prompt_time < step_time) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
   if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, st);
   return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, st);
 }
@@ -189,7 +193,7 @@ int weigh(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_
   ctx_prof_tick(ctx, st, "k_cache_weights");
   CACHE_TRY(ctx, launch(k_cache_weights<T, DIM, NT, RC>, dim3((unsigned)std::min<long long>(total, 2ll * x.num_sms)), WEIGHT_THREADS, PL::SMEM, st,
                         km, c, (const T*)a->q, a->cu_rows, a->lse, weights, a->q_stride, scale_log2, a->rows, a->heads, mask_rule(a),
-                        n_text, first, count, tiles, chunks, x.status, x.wait_ns));
+                        n_text, first, count, tiles, chunks, x.status, x.wait_ns, x.extra_arrivals));
   ctx_prof_tick(ctx, st, nullptr);
   ctx_set_launches(ctx, 1);
   return FICOCO_OK;

@@ -12,6 +12,7 @@ struct CtxAccess {
   int num_sms;
   unsigned* status;                // the device status word
   unsigned long long wait_ns;      // bound of every device-side wait
+  int extra_arrivals;              // testing hook: arrivals that the softmax barriers wait for and that never come
 };
 
 // Scratch of the cache kernels: CACHE_COUNTERS counters, zero between calls (every launch leaves them so; ficoco_status

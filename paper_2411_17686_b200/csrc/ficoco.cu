@@ -295,7 +295,7 @@ extern "C" int ficoco_profile_read(ficoco_ctx* c, int index, char* name, int nam
 
 namespace ficoco {
 
-CtxAccess ctx_access(const ficoco_ctx* c) { return CtxAccess{c->device, c->num_sms, c->status, c->wait_ns}; }
+CtxAccess ctx_access(const ficoco_ctx* c) { return CtxAccess{c->device, c->num_sms, c->status, c->wait_ns, c->dbg_extra_arrivals}; }
 int ctx_cuda_error(ficoco_ctx* c, cudaError_t e) {
   c->last_cuda = (int)e;
   return FICOCO_ERR_CUDA;

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const CacheView c,
     const __nv_bfloat16* __restrict__ q, const int* __restrict__ cu, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
     long long q_stride, float scale_log2, int rows, int heads, const MaskRule mask, unsigned* __restrict__ status,
-    unsigned long long wait_ns) {
+    unsigned long long wait_ns, int extra_arrivals) {
   using PL = PromptPlan<DIM>;
   constexpr int K_ST = PL::K_ST, V_ST = PL::V_ST, V16_ST = PL::V16_ST, SC_ST = PL::SC_ST;
   extern __shared__ unsigned char prompt_raw[];
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     for (int s = 0; s < V_ST; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 2); }
     for (int s = 0; s < V16_ST; ++s) { mbar_init(&w_full[s], 2); mbar_init(&w_empty[s], 1); }
     for (int s = 0; s < SC_ST; ++s) { mbar_init(&sc_full[s], 1); mbar_init(&sc_empty[s], 16); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 8); mbar_init(&o_bar[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&s_bar[s], 1); mbar_init(&p_bar[s], 8 + extra_arrivals); mbar_init(&o_bar[s], 1); }
     mbar_init(&raw_bar, PROMPT_ROWS);
     mbar_init(&q_bar, 16);
     mbar_init(&drain_bar, 1);

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const CacheView c,
     const T* __restrict__ q, const int* __restrict__ cu, T* __restrict__ out, float* __restrict__ lse, long long q_stride,
     float scale_log2, int rows, int heads, const MaskRule mask, int* __restrict__ counters, float* __restrict__ partials,
-    unsigned* __restrict__ status, unsigned long long wait_ns) {
+    unsigned* __restrict__ status, unsigned long long wait_ns, int extra_arrivals) {
   using PL = StepPlan<DIM, NT, RB>;
   constexpr int N = PL::N, NST = PL::STAGES, NS = PL::NS, NO = PL::NO;
   extern __shared__ unsigned char step_raw[];
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
       mbar_init(&scale_bar[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&q_bar[s], 128); mbar_init(&s_bar[s], 1); mbar_init(&s_free[s], 4); mbar_init(&p_bar[s], 4);
+      mbar_init(&q_bar[s], 128); mbar_init(&s_bar[s], 1); mbar_init(&s_free[s], 4); mbar_init(&p_bar[s], 4 + extra_arrivals);
       mbar_init(&o_bar[s], 1); mbar_init(&free_bar[s], 4); mbar_init(&l_bar[s], 4);
     }
     mbar_init(&drain_bar, 1);

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
     const __grid_constant__ CUtensorMap kmap, const CacheView c, const T* __restrict__ q, const int* __restrict__ cu,
     const float* __restrict__ lse, float* __restrict__ weights, long long q_stride, float scale_log2, int rows, int heads,
     const MaskRule mask, int n_text, int first, int count, int tiles, int chunks, unsigned* __restrict__ status,
-    unsigned long long wait_ns) {
+    unsigned long long wait_ns, int extra_arrivals) {
   using PL = WeightPlan<DIM, NT, RC>;
   constexpr int N = PL::N, NST = PL::STAGES, NSC = PL::SCALES;
   extern __shared__ unsigned char weight_raw[];
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
   if (tid == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
     for (int s = 0; s < NSC; ++s) mbar_init(&sc_bar[s], 1);
-    for (int s = 0; s < 2; ++s) { mbar_init(&q_bar[s], 4); mbar_init(&q_free[s], 8); mbar_init(&s_bar[s], 1); mbar_init(&s_free[s], 4); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&q_bar[s], 4 + extra_arrivals); mbar_init(&q_free[s], 8); mbar_init(&s_bar[s], 1); mbar_init(&s_free[s], 4); }
     mbar_init(&drain_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }

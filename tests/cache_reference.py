@@ -121,31 +121,31 @@ def attention(cache, q, rows, causal=True, window=0, sinks=0, scale=None):
     r0 = 0
     for b, m in enumerate(rows):
         n = cache.lengths[b]
+        see = np.array([visible(n, n - m + i, causal, window, sinks) for i in range(m)]).reshape(m, n)
+        some = see.any(1)                                # rows that see nothing: zeros, -inf
         for h in range(heads):
             k, v, sv = cache.tokens(b, h // (heads // cache.kv))
-            for i in range(m):
-                see = visible(n, n - m + i, causal, window, sinks)
-                if not see.any():
-                    continue
-                x = qn[r0 + i, h]
-                kk, vv = k[see], v[see]
-                s = kk @ x * scale
-                top = s.max()
-                p = np.exp(s - top)
-                l = p.sum()
-                out[r0 + i, h] = p @ vv / l
-                lse[r0 + i, h] = top + math.log(l)
-                s1 = scale * (np.abs(kk) @ np.abs(x)).max()
-                w = p / l * sv[see]
-                codes = np.abs(vv) / sv[see][:, None]
-                ds = 2.0 ** -21 * s1 + 2.0 ** -21 * (1 + np.abs(s).max())
-                if bf16:
-                    ds += scale * np.abs(x).max() * np.abs(kk).sum(1).max() * 2.0 ** -17
-                a = np.abs(vv).T @ (p / l)
-                tol[r0 + i, h] = a * ((2.0 ** -8 if bf16 else 2.0 ** -22) + 2 * ds) + \
-                    (2.0 ** -22 if bf16 else 2.0 ** -27) * w.max() * codes.sum(0) + \
-                    (2.0 ** -8 if bf16 else 2.0 ** -23) * np.abs(out[r0 + i, h]) + 1e-38
-                ltol[r0 + i, h] = ds + 2.0 ** -22 * (4 + abs(lse[r0 + i, h]))
+            x = qn[r0:r0 + m, h]
+            if not some.any():
+                continue
+            s = np.where(see, x @ k.T * scale, -math.inf)[some]
+            on = see[some]
+            top = s.max(1, keepdims=True)
+            p = np.exp(s - top)
+            l = p.sum(1, keepdims=True)
+            p /= l
+            o = p @ v
+            e = top[:, 0] + np.log(l[:, 0])
+            size = np.where(on, s, 0.0)
+            ds = 2.0 ** -21 * scale * np.where(on, np.abs(x[some]) @ np.abs(k).T, 0.0).max(1) + 2.0 ** -21 * (1 + np.abs(size).max(1))
+            if bf16:
+                ds += scale * np.abs(x[some]).max(1) * np.where(on, np.abs(k).sum(1)[None], 0.0).max(1) * 2.0 ** -17
+            t = (p @ np.abs(v)) * ((2.0 ** -8 if bf16 else 2.0 ** -22) + 2 * ds)[:, None]
+            t += (2.0 ** -22 if bf16 else 2.0 ** -27) * (p * sv).max(1)[:, None] * (on @ (np.abs(v) / sv[:, None]))
+            t += (2.0 ** -8 if bf16 else 2.0 ** -23) * np.abs(o) + 1e-38
+            at = np.nonzero(some)[0] + r0
+            out[at, h], lse[at, h], tol[at, h] = o, e, t
+            ltol[at, h] = ds + 2.0 ** -22 * (4 + np.abs(e))
         r0 += m
     return out, lse, tol, ltol
 
