@@ -334,22 +334,39 @@ class PagePool:
         return out[:n].tolist(), (None if src.value < 0 else (src.value, dst.value))
 
 
+_INT32 = None           # torch.int32, once torch is loaded (a call of these takes less time than importing a module again)
+
+
 def _int32(name: str, t, n: Optional[int] = None) -> int:
     """Address of a contiguous cuda int32 tensor."""
-    import torch
-    if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda or (n is not None and t.numel() != n):
+    global _INT32
+    if _INT32 is None:
+        import torch
+        _INT32 = torch.int32
+    if t.dtype is not _INT32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
         raise ValueError(f"{name} must be a contiguous cuda int32 tensor" + (f" of {n} values" if n is not None else ""))
     return t.data_ptr()
 
 
 def _rows3(name: str, t, dim: int) -> int:
     """Row stride of [rows, heads, dim] whose last two dimensions are contiguous."""
-    if t.dim() != 3 or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [rows, heads, {dim}], got {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim:
+        raise ValueError(f"{name} must be [rows, heads, {dim}], got {tuple(shape)}")
     stride = t.stride()
-    if not t.is_cuda or (t.shape[0] > 0 and (stride[2] != 1 or (stride[1] != dim and t.shape[1] > 1))):
+    if not t.is_cuda or (shape[0] > 0 and (stride[2] != 1 or (stride[1] != dim and shape[1] > 1))):
         raise ValueError(f"{name} must be a cuda tensor with contiguous heads")
-    return stride[0] if t.shape[0] > 1 else t.shape[1] * dim
+    return stride[0] if shape[0] > 1 else shape[1] * dim
+
+
+def _new(like, shape, dtype):
+    """A contiguous tensor on the device of ``like`` (half the time of torch.empty with a shape)."""
+    import torch
+    strides, n = [], 1
+    for x in reversed(shape):
+        strides.append(n)
+        n *= x
+    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=like.device)
 
 
 class Context:
@@ -621,12 +638,12 @@ class Context:
         import torch
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
             raise ValueError("out must be contiguous, with q's shape and type")
         if lse is None:
             if want_lse:
-                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+                lse = _new(q, (a.rows, a.heads), torch.float32)
         elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous fp32 [rows, heads]")
         a.out = out.data_ptr()
@@ -649,7 +666,7 @@ class Context:
             raise ValueError("lse must be contiguous fp32 [rows, heads]")
         shape = (cache.struct.batch, q.shape[1], n_text, count)
         if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=q.device)
+            out = _new(q, shape, torch.float32)
         elif tuple(out.shape) != shape or out.dtype != torch.float32 or not out.is_contiguous():
             raise ValueError(f"out must be contiguous fp32 {shape}")
         a.lse = lse.data_ptr()
@@ -678,7 +695,7 @@ class Context:
                 to_table.stride(1) != 1:
             raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")
         if lengths is None:
-            lengths = torch.empty((cs.batch,), dtype=torch.int32, device=to_table.device)
+            lengths = _new(to_table, (cs.batch,), torch.int32)
         a = ficoco_compact_args(to_table.data_ptr(), _int32("kept", kept), _int32("cu_kept", cu_kept, cs.batch + 1),
                                 _int32("lengths", lengths, cs.batch), to_table.stride(0), to_table.shape[1], kept.numel(), first, 0)
         rc = self.lib.ficoco_cache_compact(self.h, cs, a, _current_stream(cache.device) if stream is None else stream)
