@@ -330,8 +330,11 @@ extern "C" int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, 
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
   const int log_team = team_log(c.page * c.dim / 16, COMPACT_HELD);
-  const dim3 grid((unsigned)(((long long)a->n_kept + (long long)c.batch * a->first) / c.page + 2 * c.batch),
-                  ((2 * c.kv << log_team) + PAGE_THREADS - 1) / PAGE_THREADS);
+  const long long units = ((long long)a->n_kept + (long long)c.batch * a->first) / c.page + 2 * c.batch;
+  // CTAs along the heads of a page: as few as leave every SM eight (48 gathered sequences of 32 heads in pages of 16: 153 us, with one
+  // CTA per head group 208; 16 sequences in pages of 64 14.6, with one per head group 16.5)
+  const int parts = ((2 * c.kv << log_team) + PAGE_THREADS - 1) / PAGE_THREADS;
+  const dim3 grid((unsigned)units, (unsigned)std::min<long long>(parts, std::max(1ll, (8ll * x.num_sms + units - 1) / units)));
   ctx_prof_tick(ctx, st, "k_cache_compact");
   CACHE_TRY(ctx, launch(k_cache_compact, grid, PAGE_THREADS, 0, st, c, a->to_table, a->kept, a->cu_kept, a->lengths_out,
                         a->to_stride, a->to_pages, a->n_kept, a->first, log_team, x.status));

@@ -13,9 +13,10 @@
 namespace ficoco {
 
 constexpr int PAGE_LOG = 8, PAGE_THREADS = 1 << PAGE_LOG;
-// Vectors that a thread keeps between the two passes; more are read again.  Four CTAs of 64 registers a thread per SM, and as much as
-// those take without spilling: 16 prompts of 640 rows and 32 heads 58 us with eight, 78 with four; single tokens of 64 sequences
-// 6.2 us with eight (most of them empty), 4.3 with four; 48 gathered sequences 479 with eight, 193 with four.
+// Vectors that a thread keeps between the two passes; more are read again.  As much as the registers take without spilling, four CTAs
+// per SM (three for compact): 16 prompts of 640 rows and 32 heads 53 us with eight, 78 with four; single tokens of 64 sequences 6.2 us
+// with eight (most of them empty), 4.3 with four; 48 gathered sequences 153 us with four and three CTAs, 172 with four CTAs, 211 with
+// three vectors.
 constexpr int APPEND_HELD = 8, STEP_HELD = 4, COMPACT_HELD = 4;
 
 // Largest of `v` over the team of this thread (all values >= 0).
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
   if (lane == 0) *scale = s;
 }
 
-__global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheView c, const int* __restrict__ to_table,
+__global__ void __launch_bounds__(PAGE_THREADS, 3) k_cache_compact(const CacheView c, const int* __restrict__ to_table,
                                                                const int* __restrict__ kept, const int* __restrict__ cu,
                                                                int* __restrict__ lengths_out, long long to_stride,
                                                                int to_pages, int n_kept, int first, int log_team,
@@ -189,76 +190,81 @@ __global__ void __launch_bounds__(PAGE_THREADS, 4) k_cache_compact(const CacheVi
   }
   __syncthreads();
   const int team = 1 << log_team, mine = tid >> log_team, lane = tid & (team - 1);
-  const int pair = (blockIdx.y << (PAGE_LOG - log_team)) + mine, head = pair >> 1;
-  const bool is_v = pair & 1, on = head < c.kv;
-  const int vecs = c.dim >> 4, total = on ? s1 * vecs : 0;      // vectors of 16 codes
-  const uint8_t* src = is_v ? c.v : c.k;
-  const float* scales = is_v ? c.vs : c.ks;
-  const uint32_t inv_vecs = ((1u << 20) + vecs - 1) / vecs;     // i / vecs as a product: exact for i < 2^20 / vecs, a page has 2^11
-  auto fetch = [&](int i, uint4& codes, float& s) {
-    const int row = (int)((uint32_t)i * inv_vecs >> 20);
-    const int2 f = row_from[row];
-    const size_t at = (size_t)max(f.x, 0) * c.kv + head;
-    codes = *reinterpret_cast<const uint4*>(src + ((at << c.log_page) + f.y) * c.dim + (i - row * vecs) * 16);
-    s = f.x >= 0 ? scales[at] : 0.f;
-  };
-  auto look = [&](const uint4& u4, float s) {
-    const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
-    float m = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
-      m = fmaxf(fmaxf(m, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(d.x), fabsf(d.y)));       // (a NaN key counts for nothing)
-    }
-    return m * s;
-  };
-  uint4 held[COMPACT_HELD];
-  float hs[COMPACT_HELD];
-#pragma unroll
-  for (int x = 0; x < COMPACT_HELD; ++x) {
-    const int i = lane + (x << log_team);
-    held[x] = make_uint4(0u, 0u, 0u, 0u);
-    hs[x] = 0.f;
-    if (i < total) fetch(i, held[x], hs[x]);
-  }
-  float amax = 0.f;
-#pragma unroll
-  for (int x = 0; x < COMPACT_HELD; ++x) amax = fmaxf(amax, look(held[x], hs[x]));
+  const int groups = ((2 * c.kv << log_team) + PAGE_THREADS - 1) >> PAGE_LOG;
+  // one look-up of the page and its rows for as many heads as the grid leaves to a CTA
 #pragma unroll 1
-  for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
-    uint4 u4;
-    float s;
-    fetch(i, u4, s);
-    amax = fmaxf(amax, look(u4, s));
-  }
-  amax = team_max(amax, team >> 5, warp_max);
-  if (!on) return;
-  const size_t at = (size_t)page * c.kv + head;
-  const float s = scale_of(amax), inv = 1.0f / s;
-  uint4* out = reinterpret_cast<uint4*>((is_v ? c.v : c.k) + (at << c.log_page) * c.dim);
-  auto put = [&](int i, const uint4& u4, float by) {
-    const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
-    uint32_t o[4];
+  for (int part = blockIdx.y; part < groups; part += gridDim.y) {
+    const int pair = (part << (PAGE_LOG - log_team)) + mine, head = pair >> 1;
+    const bool is_v = pair & 1, on = head < c.kv;
+    const int vecs = c.dim >> 4, total = on ? s1 * vecs : 0;      // vectors of 16 codes
+    const uint8_t* src = is_v ? c.v : c.k;
+    const float* scales = is_v ? c.vs : c.ks;
+    const uint32_t inv_vecs = ((1u << 20) + vecs - 1) / vecs;     // i / vecs as a product: exact for i < 2^20 / vecs, a page has 2^11
+    auto fetch = [&](int i, uint4& codes, float& s) {
+      const int row = (int)((uint32_t)i * inv_vecs >> 20);
+      const int2 f = row_from[row];
+      const size_t at = (size_t)max(f.x, 0) * c.kv + head;
+      codes = *reinterpret_cast<const uint4*>(src + ((at << c.log_page) + f.y) * c.dim + (i - row * vecs) * 16);
+      s = f.x >= 0 ? scales[at] : 0.f;
+    };
+    auto look = [&](const uint4& u4, float s) {
+      const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
+      float m = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {                              // exact: powers of two (their quotient alone can overflow)
-      const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
-      o[k] = to_e4m3x2(a.x * by * inv, a.y * by * inv) | to_e4m3x2(d.x * by * inv, d.y * by * inv) << 16;
+      for (int k = 0; k < 4; ++k) {
+        const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
+        m = fmaxf(fmaxf(m, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(d.x), fabsf(d.y)));       // (a NaN key counts for nothing)
+      }
+      return m * s;
+    };
+    uint4 held[COMPACT_HELD];
+    float hs[COMPACT_HELD];
+#pragma unroll
+    for (int x = 0; x < COMPACT_HELD; ++x) {
+      const int i = lane + (x << log_team);
+      held[x] = make_uint4(0u, 0u, 0u, 0u);
+      hs[x] = 0.f;
+      if (i < total) fetch(i, held[x], hs[x]);
     }
-    out[i] = make_uint4(o[0], o[1], o[2], o[3]);
-  };
+    float amax = 0.f;
 #pragma unroll
-  for (int x = 0; x < COMPACT_HELD; ++x) {
-    const int i = lane + (x << log_team);
-    if (i < total) put(i, held[x], hs[x]);
-  }
+    for (int x = 0; x < COMPACT_HELD; ++x) amax = fmaxf(amax, look(held[x], hs[x]));
 #pragma unroll 1
-  for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
-    uint4 u4;
-    float by;
-    fetch(i, u4, by);
-    put(i, u4, by);
+    for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
+      uint4 u4;
+      float s;
+      fetch(i, u4, s);
+      amax = fmaxf(amax, look(u4, s));
+    }
+    amax = team_max(amax, team >> 5, warp_max);
+    if (!on) continue;                                            // (whole teams; the barriers in between are reached by all)
+    const size_t at = (size_t)page * c.kv + head;
+    const float s = scale_of(amax), inv = 1.0f / s;
+    uint4* out = reinterpret_cast<uint4*>((is_v ? c.v : c.k) + (at << c.log_page) * c.dim);
+    auto put = [&](int i, const uint4& u4, float by) {
+      const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {                              // exact: powers of two (their quotient alone can overflow)
+        const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
+        o[k] = to_e4m3x2(a.x * by * inv, a.y * by * inv) | to_e4m3x2(d.x * by * inv, d.y * by * inv) << 16;
+      }
+      out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+    };
+#pragma unroll
+    for (int x = 0; x < COMPACT_HELD; ++x) {
+      const int i = lane + (x << log_team);
+      if (i < total) put(i, held[x], hs[x]);
+    }
+#pragma unroll 1
+    for (int i = lane + (COMPACT_HELD << log_team); i < total; i += team) {
+      uint4 u4;
+      float by;
+      fetch(i, u4, by);
+      put(i, u4, by);
+    }
+    if (lane == 0) (is_v ? c.vs : c.ks)[at] = s;
   }
-  if (lane == 0) (is_v ? c.vs : c.ks)[at] = s;
 }
 
 // One CTA per page pair and part of the page; `words` 16-byte words of codes per page, keys and values alike.
