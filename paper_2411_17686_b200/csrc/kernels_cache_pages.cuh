@@ -33,6 +33,21 @@ __device__ __forceinline__ float team_max(float v, int team_warps, float (&warp_
   return v;
 }
 
+// The largest magnitude of many vectors, as an integer (infinity and NaN are the largest): bits of fp32, or the bits of bf16 in both
+// halves of a word, two to an instruction.
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const Raw8<float>& r) {
+  const float f[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+  return top;
+}
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const Raw8<__nv_bfloat16>& r) {
+  constexpr uint32_t ABS = 0x7FFF7FFFu;
+  return __vimax3_u16x2(__vimax3_u16x2(top, r.a.x & ABS, r.a.y & ABS), r.a.z & ABS, r.a.w & ABS);
+}
+__device__ __forceinline__ uint32_t top_bits(uint32_t top, const float*) { return top; }                       // as bits of fp32
+__device__ __forceinline__ uint32_t top_bits(uint32_t top, const __nv_bfloat16*) { return max(top & 0xFFFFu, top >> 16) << 16; }
+
 template <class T, int HELD>
 __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_HELD ? 4 : 2)) k_cache_append(const CacheView c, const T* __restrict__ k, const T* __restrict__ v,
                                                               const int* __restrict__ cu, long long k_stride, long long v_stride,
@@ -77,41 +92,34 @@ __global__ void __launch_bounds__(PAGE_THREADS, (sizeof(T) == 2 || HELD == STEP_
     if (i < total) held[x].load(from_row(i, row_of(i)));
     else held[x].clear();
   }
-  uint32_t top = 0;                       // order of magnitudes as integers: infinity and NaN are the largest
-  bool bad = false;
-  auto look = [&](const Raw8<T>& raw, int i) {
-    float f[8];
-    raw.get(f);
-    uint32_t m = 0;
+  uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7FFFFFFFu);
-    if (m >= 0x7F800000u) {
-      const int row = row_of(i);
-      atomicOr(&poisoned[mine >> 1][row >> 5], 1u << (row & 31));
-      bad = true;
-    }
-    top = max(top, m);
-  };
-#pragma unroll
-  for (int x = 0; x < HELD; ++x) look(held[x], lane + (x << log_team));
+  for (int x = 0; x < HELD; ++x) top = top_of(top, held[x]);
 #pragma unroll 1
   for (int i = lane + (HELD << log_team); i < total; i += team) {
     Raw8<T> raw;
     raw.load(from_row(i, row_of(i)));
-    look(raw, i);
+    top = top_of(top, raw);
   }
-  const bool any_bad = __syncthreads_or(bad);
+  top = top_bits(top, k);
+  const bool any_bad = __syncthreads_or(top >= 0x7F800000u);
   auto is_bad = [&](int row) { return (poisoned[mine >> 1][row >> 5] >> (row & 31) & 1u) != 0; };
-  if (any_bad) {                          // rare: once more without the rows that do not count
+  if (any_bad) {                          // rare: which rows, then once more without them
+#pragma unroll 1
+    for (int i = lane; i < total; i += team) {
+      const int row = row_of(i);
+      Raw8<T> raw;
+      raw.load(from_row(i, row));
+      if (top_bits(top_of(0, raw), k) >= 0x7F800000u) atomicOr(&poisoned[mine >> 1][row >> 5], 1u << (row & 31));
+    }
+    __syncthreads();
     top = 0;
 #pragma unroll 1
     for (int i = lane; i < total; i += team) {
       const int row = row_of(i);
-      if (is_bad(row)) continue;
-      float f[8];
-      load8(from_row(i, row), f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+      Raw8<T> raw;
+      raw.load(from_row(i, row));
+      if (!is_bad(row)) top = max(top, top_bits(top_of(0, raw), k));
     }
   }
   const float amax = team_max(__uint_as_float(top), team >> 5, warp_max);
