@@ -404,10 +404,13 @@ int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, i
  * read, skipped where it would be written), a length beyond max_pages * page_size or below zero (cut), a row offset outside
  * the rows of the call (those rows are skipped), a kept index outside its sequence (replaced by 0).
  *
- * Supported: page_size 16, 32, 64 or 128; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
- * multiple of kv_heads (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a
+ * Supported: page_size 16, 32, 64 or 128; max_pages * page_size up to 2^30; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
+ * multiple of kv_heads, rows * heads below 2^31 (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a
  * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned.  Anything else returns
  * FICOCO_ERR_INVALID_ARG or FICOCO_ERR_UNSUPPORTED and launches nothing.
+ *
+ * Attention and weights wait inside their kernels (bounded, status bit 2): after a wait that ran out, calls of these two do nothing until
+ * ficoco_status has read the word.  Append, copy and compact wait for nothing and go on.
  *
  * The first attention call of a context allocates its scratch (about 5 MB, never moved afterwards) and must therefore happen outside
  * stream capture (FICOCO_ERR_CAPTURE).  Graphs captured from one context share that scratch: they must not run at the same time.
@@ -453,7 +456,7 @@ int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco
  * sees nothing gets zeros (lse -infinity).  lse (or NULL) receives the natural logarithm of the softmax's denominator.
  * Codes are used as they are; a query row and the softmax weights are split into e4m3 terms (two for bf16 rows, the weights then
  * exact to 2^-8, six for fp32), products are exact and summed in fp32.  Value codes must not be NaN (append writes none).
- * out must not overlap q.
+ * out, lse and q must not overlap.
  */
 enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };
 typedef struct ficoco_attention_args {

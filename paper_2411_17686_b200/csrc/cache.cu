@@ -51,7 +51,7 @@ int check_cache(const ficoco_cache* c, CacheView* v) {
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return FICOCO_ERR_UNSUPPORTED;
   if (c->head_dim % 16 != 0 || c->head_dim > 256 || c->kv_heads > 1024 || c->batch > 65535) return FICOCO_ERR_UNSUPPORTED;
   if ((long long)c->n_pages * c->kv_heads * c->page_size > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;   // rows of a tensor map
-  if ((long long)c->max_pages * c->page_size > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
+  if ((long long)c->max_pages * c->page_size > 1 << 30) return FICOCO_ERR_UNSUPPORTED;                 // tokens of a sequence
   v->k = (uint8_t*)c->k_codes; v->v = (uint8_t*)c->v_codes; v->ks = c->k_scale; v->vs = c->v_scale;
   v->table = c->page_table; v->len = c->lengths; v->table_stride = c->table_stride;
   v->n_pages = c->n_pages; v->page = c->page_size; v->kv = c->kv_heads; v->dim = c->head_dim;
@@ -79,7 +79,8 @@ int check_attention(const ficoco_cache* c, const ficoco_attention_args* a) {
   return FICOCO_OK;
 }
 MaskRule mask_rule(const ficoco_attention_args* a) {
-  return MaskRule{a->window, a->window > 0 ? a->sinks : 0, (a->flags & FICOCO_CAUSAL) ? 1 : 0};
+  // (a window of 2^30 hides nothing: no sequence is longer)
+  return MaskRule{std::min(a->window, 1 << 30), a->window > 0 ? a->sinks : 0, (a->flags & FICOCO_CAUSAL) ? 1 : 0};
 }
 
 #define CACHE_TRY(ctx, expr)                                  \
@@ -239,6 +240,10 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   if ((a->rows > 0 && !a->out) || !aligned16(a->out)) return FICOCO_ERR_INVALID_ARG;
   const size_t es = a->dtype == FICOCO_BF16 ? 2 : 4, width = (size_t)a->heads * c.dim;
   if (a->rows > 0 && overlap(a->out, a->rows * width * es, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es))
+    return FICOCO_ERR_INVALID_ARG;
+  const size_t lse_bytes = (size_t)a->rows * a->heads * 4;
+  if (a->rows > 0 && a->lse && (((uintptr_t)a->lse & 3) || overlap(a->lse, lse_bytes, a->out, a->rows * width * es) ||
+                                overlap(a->lse, lse_bytes, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es)))
     return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -89,15 +89,7 @@ __device__ __forceinline__ uint2 to_e4m3x8(const float (&f)[8]) {
 }
 constexpr uint32_t E4M3_NAN4 = 0x7F7F7F7Fu;
 
-// Eight consecutive elements of a row as fp32.
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[8]) {
-  unpack(*reinterpret_cast<const uint4*>(p), f, p);
-}
-// The same as it lies in memory, for loads that are to be in flight together.
+// Eight consecutive elements of a row as they lie in memory, for loads that are to be in flight together.
 template <class T> struct Raw8;
 template <> struct Raw8<float> {
   float4 a, b;

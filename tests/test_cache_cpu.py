@@ -77,7 +77,7 @@ def test_caches_that_are_refused(lib, over, code):
     (dict(heads=0), -1), (dict(heads=5, q_stride=640), -1), (dict(q_stride=511), -1), (dict(q_stride=513), -1), (dict(scale=0.0), -1),
     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(window=-1), -1), (dict(sinks=-1), -1),
     (dict(flags=2), -1), (dict(dtype=2), -2), (dict(out=P16 * 1000), -1), (dict(out=P16 * 1000 + 1024 * 4 + 16), -1),
-    (dict(heads=65536 * 2, q_stride=65536 * 256), -2),
+    (dict(heads=65536 * 2, q_stride=65536 * 256), -2), (dict(rows=1 << 30, out=1 << 62), -2),
 ])
 def test_attention_calls_that_are_refused(lib, over, code):
     assert lib.ficoco_cache_attention(FAKE, cache(), attention(**over), None) == code
@@ -87,6 +87,8 @@ def test_attention_calls_that_are_refused(lib, over, code):
 
 def test_other_calls_that_are_refused(lib):
     c = cache()
+    for lse in (P16 * 3000 + 2, P16 * 2000 + 64, P16 * 1000 + 1024 * 4 + 1020):
+        assert lib.ficoco_cache_attention(FAKE, c, attention(lse=lse), None) == -1
     assert lib.ficoco_cache_attention(None, c, attention(), None) == -1
     assert lib.ficoco_cache_attention(FAKE, None, attention(), None) == -1
     assert lib.ficoco_cache_attention(FAKE, c, None, None) == -1

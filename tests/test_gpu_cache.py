@@ -200,6 +200,28 @@ def test_attention_fused_rows_padding_and_out_buffers(ctx):
         assert ctx.ficoco_status() == 0
 
 
+def test_strided_tables_and_windows_that_hide_nothing(ctx):
+    """A table cut out of a wider one; the largest window and more sinks than tokens are no mask, also with more rows than tokens."""
+    rng = np.random.default_rng(13)
+    for heads, kv, rows in ((4, 2, [1, 40]), (16, 8, [300, 300])):
+        cache = R.Cache(rng, [400, 30], 32, kv, 128)
+        dc = cache.device()
+        wide = torch.full((2, dc.page_table.shape[1] + 7), -3, dtype=torch.int32, device=DEV)
+        wide[:, 4:4 + dc.page_table.shape[1]] = dc.page_table
+        dc = binding.PagedCache(dc.k_codes, dc.v_codes, dc.k_scale, dc.v_scale, wide[:, 4:4 + dc.page_table.shape[1]], dc.lengths)
+        q = rows_of(rng, rows, heads, 128, "bf16")
+        cu = R.cu(rows)
+        a = ctx.ficoco_cache_attention(dc, q, cu)
+        assert torch.equal(a, ctx.ficoco_cache_attention(dc, q, cu, window=2 ** 31 - 1))
+        assert torch.equal(a, ctx.ficoco_cache_attention(dc, q, cu, window=2 ** 31 - 1, sinks=2 ** 31 - 1))
+        want, _, tol, _ = R.attention(cache, q, rows)
+        assert (np.abs(a.double().cpu().numpy() - want) <= tol).all()
+        want, _, tol, _ = R.attention(cache, q, rows, window=1, sinks=10 ** 6)
+        got = ctx.ficoco_cache_attention(dc, q, cu, window=1, sinks=2 ** 31 - 1)
+        assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+        assert ctx.ficoco_status() == 0
+
+
 def test_attention_same_bits_again_and_on_another_stream(ctx):
     rng = np.random.default_rng(5)
     cache = R.Cache(rng, [3000, 500, 17], 32, 2, 128)
