@@ -66,6 +66,24 @@ __device__ __forceinline__ void ctmem_ld16(uint32_t taddr, float* f) {
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr) : "memory");
 }
+// mbar_wait by a whole converged warp.  Every decision is a vote, so that the loop is a uniform one: lanes that leave a loop by
+// themselves have to be brought together again, which costs more than the wait where the phase is complete.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
+  const uint32_t a = smem_u32(bar);
+  unsigned long long t0 = 0;
+  for (;;) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(a), "r"(parity) : "memory");
+    if (__all_sync(0xFFFFFFFFu, done != 0)) return true;
+    const unsigned long long t = sm_cycles();
+    if (t0 == 0) t0 = t;
+    else if (__any_sync(0xFFFFFFFFu, t - t0 > 2 * limit_ns)) return false;
+  }
+}
 // An arrival that promises nothing about memory: for handing back what was only read (tensor memory behind its wait), by
 // threads with global stores in flight.  The ordinary, releasing arrival waits for those, 900 cycles and more.
 __device__ __forceinline__ void mbar_arrive_relaxed(uint64_t* bar) {

@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
   const int n_tiles = max(nt[0], nt[1]);
   auto token0 = [&](int k) { return (k < t_sink ? k : k - t_sink + t0) * CTILE; };
   bool ok = true;                                      // the same in all lanes of a warp
-  auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
+  auto wait = [&](uint64_t* bar, int phase) { ok = ok && warp_wait(bar, (uint32_t)phase & 1u, wait_ns); };
 
   if (warp == 18) {
     // ---------------- TMA and page scales: lane p brings page p of a tile -----------------------------------------------

@@ -20,6 +20,10 @@
 // Roles: warps 0-3 softmax (thread = token of the tile), warps 4-7 queries and output (thread = dimension), warp 8 TMA and
 // page scales, warp 9 MMA.  Tile i's scores are computed while tile i - 1's weights are multiplied; keys are given back as
 // soon as the scores exist; queries are two items ahead, page indexes two and scales one batch of 32 / (pages per tile) tiles.
+//
+// Measured (bf16, heads of 128): 32 sequences of 4096 tokens and 8 heads 54 us, 5.0 TB/s; 64 ragged ones of 64 to 8192 tokens 62 us, 3.4
+// TB/s; a window of 8000 tokens of 8 sequences 37 us; one sequence of 640 tokens and 32 heads 12.4 us; one tile 8.4 us, which is what start
+// and end of a CTA take.  fp32 rows, one sequence of 65536 tokens: 55 us, 2.4 TB/s.
 #pragma once
 #include "cache_umma.cuh"
 
@@ -264,7 +268,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
   const uint32_t tmem = tmem_s;
   if (dead_s) walk.left = 0;
   bool ok = true;                                      // the same in all lanes of a warp
-  auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
+  auto wait = [&](uint64_t* bar, int phase) { ok = ok && warp_wait(bar, (uint32_t)phase & 1u, wait_ns); };
 
   if (warp == 8) {
     // ---------------- TMA.  Lane = (tile of a batch, page of the tile) -------------------------------------------------------

@@ -10,6 +10,9 @@
 // left the memory idle a third of the time: 39 us for 16 sequences of 64 x 576 weights and 32 heads).
 // Roles: warps 0-3 and 4-7 output, every other tile each (thread = token), warps 8-11 queries, warp 12 TMA and key scales, warp 13
 // MMA.
+//
+// Measured: 16 sequences, 64 text rows over 576 tokens, 32 heads, bf16 (75 MB of results, 38 MB of keys): 35 us; the stores alone 16.5.  One
+// sequence of 37 over 2880, fp32, 32 heads on 8: 14.4 us.
 #pragma once
 #include "cache_umma.cuh"
 
@@ -82,7 +85,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
     return true;
   };
   bool ok = true;                                      // the same in all lanes of a warp
-  auto wait = [&](uint64_t* bar, int phase) { ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)phase & 1u, wait_ns)); };
+  auto wait = [&](uint64_t* bar, int phase) { ok = ok && warp_wait(bar, (uint32_t)phase & 1u, wait_ns); };
   // x / n_text as a product: ceil(2^32 / n_text), exact while x * n_text < 2^32 (the host sees to that); 1 gives 2^32 = 0
   const uint32_t inv_text = n_text == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)n_text + 1u;
   // row x of a head group: text row x % n_text of the last n_text, head x / n_text of the group, so that its weights lie
