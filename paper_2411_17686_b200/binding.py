@@ -236,6 +236,18 @@ class VResult:
     out_rows: List[int]   # output rows per image
 
 
+_torch = None
+
+
+def _load_torch():
+    """torch, imported by the first call that needs it (an import statement in each of the cache's calls took a twentieth of them)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 class PagedCache:
     """The 8-bit paged key/value cache of one decoder layer: tensors that the caller owns, described once.
 
@@ -244,7 +256,7 @@ class PagedCache:
     strided); ``lengths``: cuda int32 [batch].  Their contents may change between calls, the tensors may not: a cache with other
     tensors is another ``PagedCache``."""
 
-    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "page_table", "lengths", "struct", "device")
+    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "page_table", "lengths", "struct", "device", "scale")
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, lengths):
         import torch
@@ -270,6 +282,7 @@ class PagedCache:
         self.struct = ficoco_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                    page_table.data_ptr(), lengths.data_ptr(), page_table.stride(0), n_pages, page_size,
                                    kv_heads, head_dim, page_table.shape[0], page_table.shape[1])
+        self.scale = head_dim ** -0.5
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, page_size: int, head_dim: int, batch: int, max_pages: int,
@@ -334,16 +347,9 @@ class PagePool:
         return out[:n].tolist(), (None if src.value < 0 else (src.value, dst.value))
 
 
-_INT32 = None           # torch.int32, once torch is loaded (a call of these takes less time than importing a module again)
-
-
 def _int32(name: str, t, n: Optional[int] = None) -> int:
     """Address of a contiguous cuda int32 tensor."""
-    global _INT32
-    if _INT32 is None:
-        import torch
-        _INT32 = torch.int32
-    if t.dtype is not _INT32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
+    if t.dtype is not _load_torch().int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
         raise ValueError(f"{name} must be a contiguous cuda int32 tensor" + (f" of {n} values" if n is not None else ""))
     return t.data_ptr()
 
@@ -361,12 +367,11 @@ def _rows3(name: str, t, dim: int) -> int:
 
 def _new(like, shape, dtype):
     """A contiguous tensor on the device of ``like`` (half the time of torch.empty with a shape)."""
-    import torch
     strides, n = [], 1
     for x in reversed(shape):
         strides.append(n)
         n *= x
-    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=like.device)
+    return _load_torch().empty_strided(shape, strides[::-1], dtype=dtype, device=like.device)
 
 
 class Context:
@@ -626,7 +631,7 @@ class Context:
         self._same_device(cache, q)
         stride = _rows3("q", q, cs.head_dim)
         return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1), None, None, stride,
-                                     cs.head_dim ** -0.5 if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
+                                     cache.scale if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
                                      window, sinks, FICOCO_CAUSAL if causal else 0)
 
     def ficoco_cache_attention(self, cache: PagedCache, q, cu_rows, *, scale: Optional[float] = None, causal: bool = True,
@@ -635,7 +640,7 @@ class Context:
         """Attention of q (cuda [rows, heads, head_dim], the last tokens of the sequences) over the cache.  Returns out, or
         (out, lse) with want_lse.  scale: 1 / sqrt(head_dim) by default; window / sinks: a row sees the last ``window`` tokens up to
         its own and the first ``sinks``."""
-        import torch
+        torch = _load_torch()
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -643,7 +648,7 @@ class Context:
             raise ValueError("out must be contiguous, with q's shape and type")
         if lse is None:
             if want_lse:
-                lse = _new(q, (a.rows, a.heads), torch.float32)
+                lse = torch.empty_strided((a.rows, a.heads), (a.heads, 1), dtype=torch.float32, device=cache.device)
         elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous fp32 [rows, heads]")
         a.out = out.data_ptr()
@@ -660,7 +665,7 @@ class Context:
         """fp32 [batch, heads, n_text, count]: what the last n_text rows of every sequence give the ``count`` tokens from
         ``first`` on.  q, cu_rows and the mask are those of the attention call that returned lse; the result is ``attn_t2v`` of
         ``ficoco_l_reduce``."""
-        import torch
+        torch = _load_torch()
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous fp32 [rows, heads]")
@@ -688,7 +693,7 @@ class Context:
                              stream: Optional[int] = None):
         """Gathers the first ``first`` tokens of every sequence and its tokens first + kept[i] into the pages of ``to_table``
         (cuda int32 [batch, pages], other pages than the cache's).  Returns the new lengths (cuda int32 [batch])."""
-        import torch
+        torch = _load_torch()
         cs = cache.struct
         self._same_device(cache, to_table)
         if to_table.dtype != torch.int32 or to_table.dim() != 2 or to_table.shape[0] != cs.batch or not to_table.is_cuda or \
