@@ -412,8 +412,8 @@ int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, i
  * Attention and weights wait inside their kernels (bounded, status bit 2): after a wait that ran out, calls of these two do nothing until
  * ficoco_status has read the word.  Append, copy and compact wait for nothing and go on.
  *
- * The first attention call of a context allocates its scratch (about 5 MB, never moved afterwards) and must therefore happen outside
- * stream capture (FICOCO_ERR_CAPTURE).  Graphs captured from one context share that scratch: they must not run at the same time.
+ * The first attention call of a context with head_dim 64 or 128 allocates its scratch (about 5 MB, never moved afterwards) and must
+ * therefore happen outside stream capture (FICOCO_ERR_CAPTURE).  Graphs captured from one context share that scratch: they must not run at the same time.
  */
 typedef struct ficoco_cache {
   void* k_codes;           /* device e4m3 [n_pages, kv_heads, page_size, head_dim] */
@@ -455,7 +455,8 @@ int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco
  * j < lengths[b], and with FICOCO_CAUSAL j <= pos_i, and with window > 0 j > pos_i - window or j < sinks.  A row that
  * sees nothing gets zeros (lse -infinity).  lse (or NULL) receives the natural logarithm of the softmax's denominator.
  * Codes are used as they are; a query row and the softmax weights are split into e4m3 terms (two for bf16 rows, the weights then
- * exact to 2^-8, six for fp32), products are exact and summed in fp32.  Value codes must not be NaN (append writes none).
+ * exact to 2^-8, six for fp32; where a call has many bf16 rows, a weight is one fp16 number instead), products are exact and summed
+ * in fp32.  Value codes must not be NaN (append writes none).
  * out, lse and q must not overlap.
  */
 enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };

@@ -133,13 +133,11 @@ size_t scratch_bytes(const CtxAccess& x) {
 }
 
 template <class T, int DIM, int NT, int RB>
-int attend_step(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
+int attend_step(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, int* counters,
+                float* partials, cudaStream_t st) {
   using PL = StepPlan<DIM, NT, RB>;
   static_assert(PL::PART <= StepPlan<128, 2, 16>::PART, "the scratch holds it");
-  int* counters;
-  float* partials;
-  int rc = ctx_cache_scratch(ctx, st, scratch_bytes(x), &counters, &partials);
-  if (rc) return rc;
+  int rc;
   CUtensorMap km, vm;
   if ((rc = code_map(ctx, c, c.k, &km)) || (rc = code_map(ctx, c, c.v, &vm))) return rc;
   CACHE_TRY(ctx, cudaFuncSetAttribute(k_cache_step<T, DIM, NT, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM));
@@ -169,15 +167,20 @@ int attend_prompt(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const
 }
 template <int DIM>
 int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
-  if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, st);
+  int* counters;
+  float* partials;
+  // (also where a prompt needs none: so the first call, whatever its rows, is the one that allocates)
+  const int rc = ctx_cache_scratch(ctx, st, scratch_bytes(x), &counters, &partials);
+  if (rc) return rc;
+  if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, counters, partials, st);
   const long long rows = (long long)a->rows * (a->heads / c.kv);       // of all sequences, per key/value head
   // The prompt kernel takes 256 rows per CTA and needs about 5000 cycles for a tile of tokens, one CTA per SM; the step kernel takes 16
   // rows per item, two CTAs per SM, about 3000 cycles a tile: whichever has the shorter line (the tiles per row are the same).
   const long long prompt_ctas = std::max(1ll, rows / PROMPT_ROWS) * c.kv, step_items = (rows / 16 + 1) * c.kv;
   const long long prompt_time = (prompt_ctas + x.num_sms - 1) / x.num_sms * 5000, step_time = step_items * 3000 / (2 * x.num_sms);
   if (rows > 32ll * c.batch && prompt_time < step_time) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
-  if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, st);
-  return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, st);
+  if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, counters, partials, st);
+  return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, counters, partials, st);
 }
 
 template <class T, int DIM, int NT, int RC>

@@ -192,8 +192,9 @@ __global__ void __launch_bounds__(PAGE_THREADS, 3) k_cache_compact(const CacheVi
     int pos = i;
     if (i >= front) {
       const int e = kept[r.x + i - front];
-      pos = front + e;
-      if (e < 0 || pos >= len) { atomicOr(status, STATUS_CACHE); pos = 0; }
+      const bool inside = e >= 0 && e < len - front;             // (front + e alone can pass 32 bits)
+      if (!inside) atomicOr(status, STATUS_CACHE);
+      pos = inside ? front + e : 0;
     }
     // a sequence without tokens has nothing to gather, not even token 0: zeros (page -1)
     row_from[tid] = make_int2(len > 0 ? cache_page(c, b, pos >> c.log_page, 0, status) : -1, pos & (c.page - 1));

@@ -462,6 +462,13 @@ def test_what_only_the_device_can_see(ctx):
         for kept in ([5, -1], [5, 200]):
             ctx.ficoco_cache_compact(dc, to, t(kept), t([0, 1, 2]))
             assert ctx.ficoco_status() == 16
+        # kept indices whose sum with `first` passes 32 bits: token 0 in their place, as for every other one outside
+        for e in ((1 << 31) - 1, (1 << 31) - 8, -(1 << 31)):
+            ctx.ficoco_cache_compact(dc, to, t([0, e]), t([0, 1, 2]), first=8)
+            assert ctx.ficoco_status() == 16
+            page, first_page = int(cache.spare[1]), int(dc.page_table[1, 0])
+            same = dc.k_codes[page, :, 8].view(torch.uint8) == dc.k_codes[page, :, 0].view(torch.uint8)
+            assert bool(same.all()) and bool((dc.k_codes[first_page, :, 0].view(torch.uint8) != 0).any()), e
         ctx.ficoco_cache_compact(dc, t([[1 << 20], [-1]]), t([1, 2]), t([0, 1, 2]))
         assert ctx.ficoco_status() == 16
         ctx.ficoco_cache_compact(dc, to, t([1, 2]), t([0, 1, 70000]))
@@ -649,6 +656,30 @@ def test_first_attention_of_a_context_is_refused_under_capture():
         with torch.cuda.graph(torch.cuda.CUDAGraph()):
             c.ficoco_cache_attention(dc, q, cu, out=out)
         assert torch.isfinite(a).all()
+    finally:
+        c.close()
+
+
+def test_a_prompt_prepares_the_context_for_captured_single_tokens():
+    """The first attention call allocates, whatever kernel it takes: single tokens may be captured after an eager prompt."""
+    c = binding.Context(max_tokens=1024, max_dim=128, max_batch=4, max_text=16, device=0)
+    rng = np.random.default_rng(11)
+    dc = R.Cache(rng, [2100], 64, 2, 128).device()
+    q, one = rows_of(rng, [2048], 32, 128, "bf16"), rows_of(rng, [1], 32, 128, "bf16")
+    cu, cu1, out = R.cu([2048]), R.cu([1]), torch.empty_like(one)
+    try:
+        c.ficoco_profile(True)
+        c.ficoco_cache_attention(dc, q, cu)
+        assert [name for name, _, _ in c.ficoco_profile_read()] == ["k_cache_prompt"]
+        c.ficoco_profile(False)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.ficoco_cache_attention(dc, one, cu1, out=out)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, c.ficoco_cache_attention(dc, one, cu1))
+        assert c.ficoco_status() == 0
     finally:
         c.close()
 
