@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS, 2) k_cache_weights(
         wait(&s_bar[i & 1], i >> 1);
         if (!ok) break;
         ctc_fence_after();
-        const bool edge = base < in_lo || base + CTILE > in_hi, mine = j >= first && j < first + count;
+        const bool edge = base < in_lo || base > in_hi - CTILE, mine = j >= first && j < first + count;
 #pragma unroll 1
         for (int x = 0; x < n_x; x += 16) {
           float2 s[8];                                 // sums of the terms times the page's scale, smallest term first

@@ -660,6 +660,20 @@ def test_first_attention_of_a_context_is_refused_under_capture():
         c.close()
 
 
+@pytest.mark.parametrize("dim", [128, 48])
+def test_weights_of_tokens_far_behind_the_end(ctx, dim):
+    """The last tokens that a call can name (the tile's end is 2^31) weigh nothing, whatever the last tile has left in shared memory."""
+    rng = np.random.default_rng(12)
+    dc = R.Cache(rng, [200, 64], 64, 2, dim).device()
+    q, cu = rows_of(rng, [2, 2], 4, dim, "bf16"), R.cu([2, 2])
+    _, lse = ctx.ficoco_cache_attention(dc, q, cu, want_lse=True)
+    assert ctx.ficoco_cache_weights(dc, q, lse, cu, 2, 0, 64).abs().sum() > 0
+    for first, count in (((1 << 31) - 100, 99), ((1 << 30), 300), ((1 << 31) - 2, 1)):
+        w = ctx.ficoco_cache_weights(dc, q, lse, cu, 2, first, count)
+        assert torch.equal(w, torch.zeros_like(w)), (first, count)
+    assert ctx.ficoco_status() == 0
+
+
 def test_a_prompt_prepares_the_context_for_captured_single_tokens():
     """The first attention call allocates, whatever kernel it takes: single tokens may be captured after an eager prompt."""
     c = binding.Context(max_tokens=1024, max_dim=128, max_batch=4, max_text=16, device=0)
