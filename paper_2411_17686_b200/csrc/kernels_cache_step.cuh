@@ -98,7 +98,7 @@ struct StepPlan {
   static constexpr int N = NT * RB;                                  // columns of both products
   static constexpr int HALF = CTILE * DIM;                           // keys or values of a tile
   static constexpr int Q_BYTES = (N * DIM + 1023) / 1024 * 1024, P_BYTES = N * CTILE;
-  static constexpr int ROOM = 112 * 1024 - 3072 - RB * DIM * 4;      // half an SM's shared memory, less what is static
+  static constexpr int ROOM = 109 * 1024 - RB * DIM * 4;      // half an SM's shared memory, less 3 KB and RB * DIM floats that are static
   static constexpr int STAGES_FIT = (ROOM - 1024 - 2 * (Q_BYTES + P_BYTES)) / (2 * HALF);
   static constexpr int STAGES = STAGES_FIT > 6 ? 6 : STAGES_FIT;
   static constexpr int SMEM = 1024 + STAGES * 2 * HALF + 2 * (Q_BYTES + P_BYTES);
