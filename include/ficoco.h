@@ -454,9 +454,10 @@ int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco
  * scale * q_i . k_j over the tokens j that row i sees.  With position pos_i of row i, token j is seen if
  * j < lengths[b], and with FICOCO_CAUSAL j <= pos_i, and with window > 0 j > pos_i - window or j < sinks.  A row that
  * sees nothing gets zeros (lse -infinity).  lse (or NULL) receives the natural logarithm of the softmax's denominator.
- * Codes are used as they are; a query row and the softmax weights are split into e4m3 terms (two for bf16 rows, the weights then
- * exact to 2^-8, six for fp32; where a call has many bf16 rows, a weight is one fp16 number instead), products are exact and summed
- * in fp32.  Value codes must not be NaN (append writes none).
+ * Codes are used as they are; a query row and the softmax weights are split into e4m3 terms (two for bf16 rows, six for fp32; where
+ * a call has many bf16 rows, a weight is one fp16 number instead), products are exact and summed in fp32.  Two terms hold a weight
+ * (times its page's value scale) to 2^-8 of itself, and to 2^-22 of the largest one of the 32 tokens 32 i .. 32 i + 31 around it; six to
+ * 2^-24 and 2^-38.  Value codes must not be NaN (append writes none).
  * out, lse and q must not overlap.
  */
 enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };

@@ -2,14 +2,16 @@
 //
 // Mathematics.  For a tile of 128 tokens and the RB query rows that share a key/value head, S^T = K Q^T and
 // O^T = V^T P^T: the codes are operand A of both products (128 rows: tokens, then dimensions) as TMA brought them, the few
-// query rows are the columns.  With s_j the score in units of log2 and e_j = log2 of the page's value scale, the
-// running maximum is that of t_j = s_j + e_j, the weights are P_j = 2^(t_j - max), so that codes can be summed without their scale,
-// and the denominator sums P_j / 2^e_j.  Rows and weights are split into NT e4m3 terms (cache_umma.cuh), one more block of
-// columns each.
+// query rows are the columns.  With s_j the score in units of log2 and e_j = log2 of the page's value scale, t_j = s_j + e_j
+// and the weights are P_j = 2^(t_j - max), so that codes can be summed without their scale; the denominator sums P_j / 2^e_j.  Rows
+// and weights are split into NT e4m3 terms (cache_umma.cuh), one more block of columns each.
 //
-// The maximum is a warp's own: warp w works on tokens 32 w .. 32 w + 31 of every tile, which are one K step of the second
+// The maximum is that of 32 tokens: warp w works on tokens 32 w .. 32 w + 31 of every tile, which are one K step of the second
 // product, so each step gets an accumulator of its own and the four are joined, with the factors that bring them to one
-// maximum, where they are added to the fp32 sums in registers.  No barrier stands between a tile's scores and its weights.
+// maximum, where they are added to the fp32 sums in registers.  No barrier stands between a tile's scores and its weights.  The
+// 8-bit terms end 2^-22 (six terms: 2^-38) below what they are relative to, so that a running maximum would lose the tokens behind
+// a dominant one (a first token with nearly all of the weight and a value near zero: behind a score 16 above theirs the warp that had it lost
+// all of its tokens, a quarter of the result); relative to 32 neighbours, of them alone.  The denominator, in fp32, keeps a running maximum per warp.
 //
 // What bounds it: HBM, one byte per key or value element.  The tensor cores are idle most of the time and nothing is
 // converted, so an SM needs about 200 instructions per warp and tile of 32 KB.  All tiles of all (sequence, row block, head)
@@ -25,6 +27,7 @@
 // TB/s; a window of 8000 tokens of 8 sequences 37 us; one sequence of 640 tokens and 32 heads 12.4 us; one tile 8.4 us, which is what start
 // and end of a CTA take.  fp32 rows, one sequence of 65536 tokens: 55 us, 2.4 TB/s.
 #pragma once
+#include <float.h>
 #include "cache_umma.cuh"
 
 namespace ficoco {
@@ -98,7 +101,8 @@ struct StepPlan {
   static constexpr int N = NT * RB;                                  // columns of both products
   static constexpr int HALF = CTILE * DIM;                           // keys or values of a tile
   static constexpr int Q_BYTES = (N * DIM + 1023) / 1024 * 1024, P_BYTES = N * CTILE;
-  static constexpr int ROOM = 109 * 1024 - RB * DIM * 4;      // half an SM's shared memory, less 3 KB and RB * DIM floats that are static
+  // half an SM's shared memory, less what is static: RB * DIM floats, 288 bytes per row and 768
+  static constexpr int ROOM = 112 * 1024 - RB * (DIM * 4 + 288) - 768;
   static constexpr int STAGES_FIT = (ROOM - 1024 - 2 * (Q_BYTES + P_BYTES)) / (2 * HALF);
   static constexpr int STAGES = STAGES_FIT > 6 ? 6 : STAGES_FIT;
   static constexpr int SMEM = 1024 + STAGES * 2 * HALF + 2 * (Q_BYTES + P_BYTES);
@@ -168,9 +172,9 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
   __shared__ uint64_t q_bar[2], s_bar[2], s_free[2], p_bar[2], o_bar[2], free_bar[2], l_bar[2], drain_bar;
   __shared__ uint32_t tmem_s;
   __shared__ float page_scale[NST][3][8];              // key scale, log2 of the value scale, 1 / value scale
-  __shared__ float wmax[2][4][RB];                     // running maxima of the softmax warps, behind a tile
+  __shared__ float wmax[2][4][RB];                     // a tile's maxima per softmax warp, which its weights are relative to
   __shared__ __align__(16) float factor[2][4][5][RB];  // per output warp: what brings the four warps' sums, and the old ones, to one maximum
-  __shared__ float l_s[2][4][RB];                      // denominators of an item, per softmax warp
+  __shared__ float l_s[2][4][RB], m_s[2][4][RB];       // denominators of an item per softmax warp, and the maxima that they are relative to
   __shared__ float q_scale[2][RB];
   __shared__ int2 row_see[2][RB];                      // tokens [x, y) of a row (and its sinks)
   __shared__ StepSeg seg_s[4];                         // the output warps' items: this one and the two ahead
@@ -432,9 +436,9 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
     for (int seg = 0; ok && step_next(walk, g, c, cu, rows, group, RB, mask, status); ++seg) {
       const int buf_q = seg & 1;
       wait(&q_bar[buf_q], seg >> 1);                           // the rows' scales and masks
-      float m[RB], l[RB];
+      float m[RB], l[RB];                                      // the warp's largest so far, the denominators relative to it
 #pragma unroll
-      for (int r = 0; r < RB; ++r) { m[r] = -CUDART_INF_F; l[r] = 0.f; }
+      for (int r = 0; r < RB; ++r) { m[r] = -FLT_MAX; l[r] = 0.f; }
       // a tile inside [in_lo, in_hi) is seen by every row of the item
       const int i_first = (int)((uint32_t)g.block * RB / (uint32_t)group);
       const int i_last = min((int)(((uint32_t)g.block * RB + RB - 1) / (uint32_t)group), g.s.n_rows - 1);
@@ -474,18 +478,20 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
             }
           }
         }
+        float top[RB];                                         // of these 32 tokens (-FLT_MAX: none is seen)
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-          const float mn = fmaxf(m[r], warp_max(s[r])), ref = mn == -CUDART_INF_F ? 0.f : mn;
-          const float corr = ex2(m[r] - ref);
-          m[r] = mn;
-          s[r] = ex2(s[r] - ref);
-          l[r] = fmaf(l[r], corr, s[r] * vi);
+          top[r] = fmaxf(warp_max(s[r]), -FLT_MAX);
+          s[r] = ex2(s[r] - top[r]);
+          // old sum and new weight brought to the larger of the two maxima: one of the factors is 1
+          const float d = m[r] - top[r], e = ex2(-fabsf(d)), w = s[r] * vi;
+          l[r] = d > 0.f ? fmaf(w, e, l[r]) : fmaf(l[r], e, w);
+          m[r] = fmaxf(m[r], top[r]);
         }
         if (i >= 2) wait(&free_bar[buf], (i >> 1) - 1);        // the weights and maxima of tile i - 2 have been used
         if (!ok) break;
         {                                                      // (a store per row under `lane == r` took 160 cycles each)
-          const float mine_m = pick<RB>(m, lane);
+          const float mine_m = pick<RB>(top, lane);
           if (lane < RB) wmax[buf][warp][lane] = mine_m;
         }
         const uint32_t p = p_base + (uint32_t)buf * PL::P_BYTES + (tid & 15);
@@ -506,8 +512,8 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         if (++st == NST) { st = 0; ++wrap; }
       }
       if (!ok) break;
-      const float sum = warp_sums<RB>(l, lane);
-      if (lane < RB) l_s[buf_q][warp][lane] = sum;
+      const float mine_m = pick<RB>(m, lane), sum = warp_sums<RB>(l, lane);
+      if (lane < RB) { l_s[buf_q][warp][lane] = sum; m_s[buf_q][warp][lane] = mine_m; }
       __syncwarp();
       if (lane == 0) mbar_arrive(&l_bar[buf_q]);
     }
@@ -584,7 +590,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
 #pragma unroll
       for (int r = 0; r < RB; ++r) acc[r] = 0.f;
 #pragma unroll
-      for (int p = 0; p < PER; ++p) m_run[p] = -CUDART_INF_F;
+      for (int p = 0; p < PER; ++p) m_run[p] = -FLT_MAX;
 #pragma unroll 1
       for (int t = 1; t <= count; ++t, ++i) {
         const int buf = i & 1;
@@ -597,9 +603,8 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
           float mn = fmaxf(m_run[p], mw);
           mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 8));
           mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 16));
-          const float ref = mn == -CUDART_INF_F ? 0.f : mn;
-          f[w][r] = ex2(mw - ref);
-          f[4][r] = ex2(m_run[p] - ref);                         // (the same from four lanes)
+          f[w][r] = ex2(mw - mn);
+          f[4][r] = ex2(m_run[p] - mn);                          // (the same from four lanes)
           m_run[p] = mn;
         }
         __syncwarp();
@@ -627,10 +632,12 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         for (int r = 0; r < RB; ++r) out_s[r][d] = acc[r];
       }
       if (bw == 0 && lane < RB) {
-        const float (*f)[RB] = factor[(i - 1) & 1][0];
-        den_s[lane] = fmaf(l_s[buf_q][0][lane], f[0][lane], l_s[buf_q][1][lane] * f[1][lane]) +
-                      fmaf(l_s[buf_q][2][lane], f[2][lane], l_s[buf_q][3][lane] * f[3][lane]);
-        top_s[lane] = lane < 8 ? m_run[0] : m_run[PER - 1];
+        const float top = lane < 8 ? m_run[0] : m_run[PER - 1];      // (the largest of m_s)
+        float den = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) den = fmaf(l_s[buf_q][w][lane], ex2(m_s[buf_q][w][lane] - top), den);
+        den_s[lane] = den;
+        top_s[lane] = top;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&free_bar[(i - 1) & 1]);
@@ -679,7 +686,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
 #pragma unroll 1
           for (int u = bt; u < nr * (DIM / 4); u += 128) {
             const int r = u / (DIM / 4), d4 = (u % (DIM / 4)) * 4;
-            float top = -CUDART_INF_F, den = 0.f;
+            float top = -FLT_MAX, den = 0.f;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
             // eight parts at a time, in order, the sums brought to the larger maximum
 #pragma unroll 1
@@ -696,13 +703,13 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
               float mn = top;
 #pragma unroll
               for (int k = 0; k < 8; ++k) mn = fmaxf(mn, m8[k]);       // (the last part again in the places behind it)
-              const float ref = mn == -CUDART_INF_F ? 0.f : mn, w0 = ex2(top - ref);
+              const float w0 = ex2(top - mn);
               top = mn;
               den *= w0; a.x *= w0; a.y *= w0; a.z *= w0; a.w *= w0;
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
                 if (k0 + k >= parts) break;
-                const float w = ex2(m8[k] - ref);
+                const float w = ex2(m8[k] - mn);
                 den = fmaf(w, l8[k], den);
                 a.x = fmaf(w, v8[k].x, a.x); a.y = fmaf(w, v8[k].y, a.y); a.z = fmaf(w, v8[k].z, a.z); a.w = fmaf(w, v8[k].w, a.w);
               }
