@@ -5,8 +5,11 @@
 // group), so that a tile reads its keys and values once for all heads of the group.  S = Q K^T per tile of 128 tokens: the keys' codes
 // as they lie in memory against two e4m3 terms of the query rows at one scale (cache_umma.cuh).  t = log2 score + log2 of the
 // page's value scale; P = 2^(t - ref) in fp16 (2^-11, where two e4m3 terms would hold 2^-8 and cost twice the conversions), the
-// values' codes converted to fp16, which is exact; the denominator sums P / value scale in fp32.  ref follows the running maximum
-// only when that has grown by more than 2^8 since (P stays below 2^8, fp16's range is 2^16), so that O is rarely rescaled.
+// values' codes converted to fp16, which is exact; the denominator sums P / value scale in fp32.  ref lies 2^7 below the largest t
+// of a tile of tokens and is left there while a tile's largest P stays in [2^-5, 2^15] (fp16 ends at 2^16 and 2^-24), so that O is rarely
+// rescaled: fp16 holds a weight to 2^-11, and to 2^-20 of the largest one of its tile.  It follows the tiles down as well as up: behind a
+// dominant first token, whose value is near zero, a reference that stays at the running maximum loses the bits of all others (from 2^-14 of it
+// on, all of them at 2^-25).  Not further than 2^16 below the highest it was, so that sums and denominators cannot overflow.
 //
 // What bounds it: the tensor cores and the exponentials, which take about the same time: two row tiles per CTA take turns, one's
 // softmax runs under the other's products.  P lies in tensor memory in the place of the scores it came from, which spares shared
@@ -356,7 +359,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
     // a tile inside [in_lo, in_hi) is seen by every row of the warp
     const int in_hi = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32), len).z;
     const int in_lo = seen(mask, len - n_rows + query(x0 + t * 128 + wr * 32 + 31), len).y;
-    float ref = -CUDART_INF_F, l = 0.f;
+    float ref = -CUDART_INF_F, high = -CUDART_INF_F, l = 0.f;      // reference of weights, sums and l; the highest one so far
     bool alive = true;                                 // the same in a warp and its partner, who share a barrier per tile
     for (int i = 0; alive && i < n_tiles; ++i) {
       const int sc = i % SC_ST;
@@ -402,13 +405,15 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1) k_cache_prompt(
       if (cta_sync_or(pair_bar, 64, !ok)) { alive = false; ok = false; break; }
       top = fmaxf(top, half_s[half ^ 1][row]);
       // the products of the tiles before are complete: scores of this one were issued behind them
-      const bool move = top > ref + 8.f || ref == -CUDART_INF_F;
+      // (a tile that the row does not see moves nothing)
+      const bool move = top > ref + 15.f || (top < ref - 5.f && top > -CUDART_INF_F);
       if (__any_sync(0xFFFFFFFFu, move)) {
-        const float to = move ? fmaxf(top, ref) : ref;
-        const float by = to == -CUDART_INF_F ? 0.f : ex2(ref - to);
-        ref = to;
+        const float want = fmaxf(top - 7.f, high - 16.f);
+        const float by = move ? ex2(ref - want) : 1.f;
+        ref = move ? want : ref;
+        high = fmaxf(high, ref);
         l *= by;
-        if (i > 0) {
+        if (i > 0 && __any_sync(0xFFFFFFFFu, by != 1.f)) {
 #pragma unroll 1
           for (int cc = 0; cc < DIM / 2; cc += 16) {
             float o[16];

@@ -136,3 +136,26 @@ def test_the_tail_behind_a_sink_whose_page_has_a_larger_scale(ctx, dtype):
     out, lse = ctx.ficoco_cache_attention(dc, q.repeat(copies, 1, 1), R.cu([1] * copies), want_lse=True)
     assert ctx.ficoco_status() == 0
     compare(out[-1:], lse[-1:], *expected(cache, q, "step"))
+
+
+# dim, page, heads, kv, tokens, rows, above, sinks, mask
+PROMPTS = [
+    (128, 64, 16, 8, 12000, 520, 16.0, 1, {}),
+    (128, 16, 16, 8, 9000, 530, 18.0, 1, {}),
+    (64, 128, 16, 8, 12000, 520, 17.0, 4, {}),
+    (128, 64, 16, 8, 12000, 520, 16.0, 4, dict(window=9000, sinks=4)),
+    (128, 32, 16, 8, 6000, 520, 24.0, 1, dict(causal=False)),
+]
+
+
+@pytest.mark.parametrize("dim,page,heads,kv,n,rows,above,sinks,mask", PROMPTS)
+def test_the_tail_behind_a_sink_prompts(ctx, dim, page, heads, kv, n, rows, above, sinks, mask):
+    rng = np.random.default_rng(n + heads + dim)
+    cache, u = sunk(rng, n, page, kv, dim, above, sinks)
+    q = torch.from_numpy(u + 0.1 * rng.standard_normal((rows, heads, dim))).to(torch.bfloat16).to(DEV)
+    ctx.ficoco_profile(True)
+    out, lse = ctx.ficoco_cache_attention(cache.device(), q, R.cu([rows]), want_lse=True, **mask)
+    assert [name for name, _, _ in ctx.ficoco_profile_read()] == ["k_cache_prompt"]
+    ctx.ficoco_profile(False)
+    assert ctx.ficoco_status() == 0
+    compare(out, lse, *expected(cache, q, "prompt", **mask))
