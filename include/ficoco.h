@@ -458,8 +458,8 @@ int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco
  * a call has many bf16 rows, a weight is one fp16 number instead), products are exact and summed in fp32.  Two terms hold a weight
  * (times its page's value scale) to 2^-8 of itself, and to 2^-22 of the largest one of the 32 tokens 32 i .. 32 i + 31 around it; six to
  * 2^-24 and 2^-38; fp16 to 2^-11 and to 2^-20 of the largest one of its 128 tokens 128 i .. 128 i + 127 (2^-48 of the row's largest, if
- * that is more).  Two terms hold a bf16 query element exactly down to 2^-14 of its row's largest one, where a call has many rows down to
- * 2^-10, and smaller ones to 2^-22 and 2^-17 of that.  Value codes must not be NaN (append writes none).
+ * that is more).  Two terms hold a bf16 query element exactly down to 2^-13 of its row's largest one, where a call has many rows down to
+ * 2^-9, and smaller ones to 2^-21 and 2^-17 of that.  Value codes must not be NaN (append writes none).
  * out, lse and q must not overlap.
  */
 enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };
