@@ -347,10 +347,12 @@ class PagePool:
         return out[:n].tolist(), (None if src.value < 0 else (src.value, dst.value))
 
 
-def _int32(name: str, t, n: Optional[int] = None) -> int:
-    """Address of a contiguous cuda int32 tensor."""
-    if t.dtype is not _load_torch().int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
-        raise ValueError(f"{name} must be a contiguous cuda int32 tensor" + (f" of {n} values" if n is not None else ""))
+def _int32(name: str, t, n: Optional[int] = None, device=None) -> int:
+    """Address of a contiguous cuda int32 tensor, on ``device`` if one is given."""
+    if t.dtype is not _load_torch().int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n) or \
+            (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a contiguous cuda int32 tensor" + (f" of {n} values" if n is not None else "") +
+                         (f" on {device}" if device is not None else ""))
     return t.data_ptr()
 
 
@@ -616,7 +618,7 @@ class Context:
         self._same_device(cache, k)
         if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.shape[1:] != (cs.kv_heads, cs.head_dim):
             raise ValueError(f"k and v must both be [rows, {cs.kv_heads}, {cs.head_dim}] of one type")
-        a = ficoco_append_args(k.data_ptr(), v.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1),
+        a = ficoco_append_args(k.data_ptr(), v.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1, cache.device),
                                _rows3("k", k, cs.head_dim), _rows3("v", v, cs.head_dim), _dtype_code(k), k.shape[0])
         rc = self.lib.ficoco_cache_append(self.h, cs, a, _current_stream(cache.device) if stream is None else stream)
         if rc:
@@ -630,7 +632,7 @@ class Context:
         cs = cache.struct
         self._same_device(cache, q)
         stride = _rows3("q", q, cs.head_dim)
-        return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1), None, None, stride,
+        return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1, cache.device), None, None, stride,
                                      cache.scale if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
                                      window, sinks, FICOCO_CAUSAL if causal else 0)
 
@@ -644,13 +646,13 @@ class Context:
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
-            raise ValueError("out must be contiguous, with q's shape and type")
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or out.device != cache.device:
+            raise ValueError("out must be contiguous, with q's shape, type and device")
         if lse is None:
             if want_lse:
                 lse = torch.empty_strided((a.rows, a.heads), (a.heads, 1), dtype=torch.float32, device=cache.device)
-        elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("lse must be contiguous fp32 [rows, heads]")
+        elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != cache.device:
+            raise ValueError("lse must be contiguous fp32 [rows, heads] on q's device")
         a.out = out.data_ptr()
         if lse is not None:
             a.lse = lse.data_ptr()
@@ -667,13 +669,13 @@ class Context:
         ``ficoco_l_reduce``."""
         torch = _load_torch()
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
-        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("lse must be contiguous fp32 [rows, heads]")
+        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != cache.device:
+            raise ValueError("lse must be contiguous fp32 [rows, heads] on q's device")
         shape = (cache.struct.batch, q.shape[1], n_text, count)
         if out is None:
             out = _new(q, shape, torch.float32)
-        elif tuple(out.shape) != shape or out.dtype != torch.float32 or not out.is_contiguous():
-            raise ValueError(f"out must be contiguous fp32 {shape}")
+        elif tuple(out.shape) != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.device != cache.device:
+            raise ValueError(f"out must be contiguous fp32 {shape} on q's device")
         a.lse = lse.data_ptr()
         rc = self.lib.ficoco_cache_weights(self.h, cache.struct, a, n_text, first, count, out.data_ptr(),
                                            _current_stream(cache.device) if stream is None else stream)
@@ -684,7 +686,8 @@ class Context:
     def ficoco_cache_copy(self, cache: PagedCache, src, dst, *, stream: Optional[int] = None) -> None:
         """Copies page src[i] to page dst[i] (cuda int32 tensors of one length; pairs with a negative page are skipped)."""
         self._same_device(cache, src)
-        rc = self.lib.ficoco_cache_copy(self.h, cache.struct, _int32("src", src), _int32("dst", dst, src.numel()), src.numel(),
+        rc = self.lib.ficoco_cache_copy(self.h, cache.struct, _int32("src", src),
+                                        _int32("dst", dst, src.numel(), cache.device), src.numel(),
                                         _current_stream(cache.device) if stream is None else stream)
         if rc:
             _check(self.h, rc)
@@ -701,8 +704,9 @@ class Context:
             raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")
         if lengths is None:
             lengths = _new(to_table, (cs.batch,), torch.int32)
-        a = ficoco_compact_args(to_table.data_ptr(), _int32("kept", kept), _int32("cu_kept", cu_kept, cs.batch + 1),
-                                _int32("lengths", lengths, cs.batch), to_table.stride(0), to_table.shape[1], kept.numel(), first, 0)
+        a = ficoco_compact_args(to_table.data_ptr(), _int32("kept", kept, None, cache.device),
+                                _int32("cu_kept", cu_kept, cs.batch + 1, cache.device),
+                                _int32("lengths", lengths, cs.batch, cache.device), to_table.stride(0), to_table.shape[1], kept.numel(), first, 0)
         rc = self.lib.ficoco_cache_compact(self.h, cs, a, _current_stream(cache.device) if stream is None else stream)
         if rc:
             _check(self.h, rc)

@@ -1,0 +1,89 @@
+"""Refusals of the 8-bit cache's calls, without a GPU: tensors that lie on another device than the cache."""
+import types
+
+import pytest
+import torch
+
+from paper_2411_17686_b200 import binding
+
+GPU, OTHER, CPU = torch.device("cuda", 0), torch.device("cuda", 1), torch.device("cpu")
+
+
+class Shown:
+    """What the binding looks at in a tensor, on a device that need not exist."""
+
+    def __init__(self, shape, dtype, device=GPU):
+        self.shape, self.dtype, self.device, self.is_cuda = torch.Size(shape), dtype, device, device.type == "cuda"
+
+    def stride(self, d=None):
+        s = [1]
+        for n in reversed(self.shape[1:]):
+            s.insert(0, s[0] * n)
+        return tuple(s) if d is None else s[d]
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x10000
+
+
+class Reached(Exception):
+    pass
+
+
+class Library:
+    def __getattr__(self, name):
+        def call(*args):
+            raise Reached(name)
+        return call
+
+
+@pytest.fixture
+def ctx():
+    c = binding.Context.__new__(binding.Context)
+    c.device, c.h, c.lib = 0, None, Library()
+    return c
+
+
+BATCH, ROWS, HEADS, KV, DIM, TEXT, COUNT = 3, 5, 4, 2, 128, 2, 7
+I32, F32, BF16 = torch.int32, torch.float32, torch.bfloat16
+
+
+def tensors(**over):
+    shapes = dict(q=((ROWS, HEADS, DIM), BF16), out=((ROWS, HEADS, DIM), BF16), lse=((ROWS, HEADS), F32), k=((ROWS, KV, DIM), BF16),
+                  v=((ROWS, KV, DIM), BF16), cu=((BATCH + 1,), I32), weights=((BATCH, HEADS, TEXT, COUNT), F32), src=((6,), I32),
+                  dst=((6,), I32), to=((BATCH, 4), I32), kept=((9,), I32), lengths=((BATCH,), I32))
+    return types.SimpleNamespace(**{n: Shown(s, t, over.get(n, GPU)) for n, (s, t) in shapes.items()})
+
+
+def cache():
+    s = binding.ficoco_cache(*([0x10000] * 6), 8, 10, 64, KV, DIM, BATCH, 8)
+    return types.SimpleNamespace(struct=s, device=GPU, scale=DIM ** -0.5)
+
+
+CALLS = {
+    "append": (lambda c, t: c.ficoco_cache_append(cache(), t.k, t.v, t.cu, stream=0), ("k", "v", "cu")),
+    "attention": (lambda c, t: c.ficoco_cache_attention(cache(), t.q, t.cu, out=t.out, lse=t.lse, stream=0), ("q", "cu", "out", "lse")),
+    "weights": (lambda c, t: c.ficoco_cache_weights(cache(), t.q, t.lse, t.cu, TEXT, 0, COUNT, out=t.weights, stream=0),
+                ("q", "lse", "cu", "weights")),
+    "copy": (lambda c, t: c.ficoco_cache_copy(cache(), t.src, t.dst, stream=0), ("src", "dst")),
+    "compact": (lambda c, t: c.ficoco_cache_compact(cache(), t.to, t.kept, t.cu, lengths=t.lengths, stream=0),
+                ("to", "kept", "cu", "lengths")),
+}
+
+
+@pytest.mark.parametrize("device", [CPU, OTHER], ids=str)
+@pytest.mark.parametrize("call,name", [(c, n) for c, (_, names) in CALLS.items() for n in names])
+def test_tensors_on_another_device_are_refused(ctx, call, name, device):
+    run = CALLS[call][0]
+    with pytest.raises(Reached):                         # with everything in place the library is called
+        run(ctx, tensors())
+    with pytest.raises(ValueError):
+        run(ctx, tensors(**{name: device}))
