@@ -250,15 +250,16 @@ __global__ void __launch_bounds__(PAGE_THREADS, 3) k_cache_compact(const CacheVi
     amax = team_max(amax, team >> 5, warp_max);
     if (!on) continue;                                            // (whole teams; the barriers in between are reached by all)
     const size_t at = (size_t)page * c.kv + head;
-    const float s = scale_of(amax), inv = 1.0f / s;
+    const float s = scale_of(amax), inv2 = 2.0f / s;
     uint4* out = reinterpret_cast<uint4*>((is_v ? c.v : c.k) + (at << c.log_page) * c.dim);
     auto put = [&](int i, const uint4& u4, float by) {
       const uint32_t w[4] = {u4.x, u4.y, u4.z, u4.w};
+      const float half = 0.5f * by;
       uint32_t o[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {                              // exact: powers of two (their quotient alone can overflow)
+      for (int k = 0; k < 4; ++k) {          // exact: powers of two (their quotient alone can overflow, a value itself be 2^128 and more)
         const float2 a = from_e4m3x2(w[k] & 0xFFFFu), d = from_e4m3x2(w[k] >> 16);
-        o[k] = to_e4m3x2(a.x * by * inv, a.y * by * inv) | to_e4m3x2(d.x * by * inv, d.y * by * inv) << 16;
+        o[k] = to_e4m3x2(a.x * half * inv2, a.y * half * inv2) | to_e4m3x2(d.x * half * inv2, d.y * half * inv2) << 16;
       }
       out[i] = make_uint4(o[0], o[1], o[2], o[3]);
     };

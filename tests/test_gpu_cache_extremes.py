@@ -1,0 +1,50 @@
+"""The 8-bit cache at the ends of fp32's range and of its own limits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_17686_b200 import binding
+from tests import cache_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context(max_tokens=1024, max_dim=128, max_batch=4, max_text=16, device=0)
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_values_that_round_to_2_to_the_128(ctx, dtype):
+    """The largest finite numbers become code 256 at scale 2^120; gathered they stay what they are."""
+    big = torch.finfo(dtype).max
+    n, page, kv, dim = 40, 16, 2, 32
+    cache = R.Cache(np.random.default_rng(0), [0], page, kv, dim, spare=6, max_pages=4)
+    cache.table[0, :3], to = cache.spare[:3], cache.spare[3:5]
+    cache.lengths = [n]
+    k = torch.randn((n, kv, dim), generator=torch.Generator().manual_seed(0)).to(dtype)
+    v = k * 2.0 ** 100
+    k[[3, 20], 0, 5], k[4, 1, 6], v[[7, 25], 1, 2], v[2, 0, 1] = big, -big, -big, big
+    dc = cache.device()
+    ctx.ficoco_cache_append(dc, k.to(DEV), v.to(DEV), R.cu([n]))
+    cache.write(0, 0, k.double().numpy(), v.double().numpy())
+    kept = np.array([3, 4, 2, 7, 20, 25, 1, 39, 38, 0] + list(range(8, 20)), dtype=np.int32)
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)      # noqa: E731
+    got = ctx.ficoco_cache_compact(dc, t(to[None].astype(np.int32)), t(kept), R.cu([len(kept)]))
+    assert got.tolist() == [len(kept)] and ctx.ficoco_status() == 0
+    for pi in range(2):
+        at = kept[pi * page:(pi + 1) * page]
+        sp = cache.table[0, at // page]
+        for codes, scales in ((cache.kc, cache.ks), (cache.vc, cache.vs)):
+            for h in range(kv):
+                x = R.E4M3[codes[sp, h, at % page]] * scales[sp, h].astype(np.float64)[:, None]
+                scales[to[pi], h] = R.scale_of(np.abs(x).max())
+                codes[to[pi], h, :len(at)] = R.to_codes(x / float(scales[to[pi], h]))
+    assert cache.ks[to[0], 0] == 2.0 ** 120 and 256.0 in R.E4M3[cache.kc[to[0], 0]]
+    for got, want in ((dc.k_codes, cache.kc), (dc.v_codes, cache.vc)):
+        assert np.array_equal(got.view(torch.uint8).cpu().numpy(), want)
+    for got, want in ((dc.k_scale, cache.ks), (dc.v_scale, cache.vs)):
+        assert np.array_equal(got.cpu().numpy(), want, equal_nan=True)
