@@ -402,7 +402,8 @@ int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, i
  *
  * What only the device can see sets bit 4 (16) of the status word: a page index outside the pool (replaced by 0 where it is
  * read, skipped where it would be written), a length beyond max_pages * page_size or below zero (cut), a row offset outside
- * the rows of the call (those rows are skipped), a kept index outside its sequence (replaced by 0).
+ * the rows of the call (those rows are skipped; an attention call whose offsets go back to earlier rows so often that its work cannot be
+ * counted in 31 bits does nothing), a kept index outside its sequence (replaced by 0).
  *
  * Supported: page_size 16, 32, 64 or 128; max_pages * page_size up to 2^30; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
  * multiple of kv_heads, rows * heads below 2^31 (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a

@@ -207,6 +207,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
   int total = 0, n_cta, piece0;
   {
     int nt_most = 0, size = 0;
+    long long sum = 0;
     StepSeq s0;
 #pragma unroll 1
     for (int b0 = 0; b0 < c.batch; b0 += 32) {
@@ -216,9 +217,16 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_cache_step(
         size = s0.blocks * c.kv * s0.nt;
         if (size > 0) nt_most = max(nt_most, s0.nt);
       }
-      total += size;
+      sum += size;
     }
-    total = __reduce_add_sync(0xFFFFFFFFu, total);
+    // The host keeps the list below 2^31 tiles for sequences that share no row.  Offsets that go back to rows of earlier sequences can
+    // make it longer: no place in it could be trusted then.
+    if (__reduce_add_sync(0xFFFFFFFFu, (uint32_t)min(sum >> 16, 1ll << 26)) >= (1u << 15) - 32) {
+      if (lane == 0) atomicOr(status, STATUS_CACHE);
+      sum = 0;
+      nt_most = 0;
+    }
+    total = __reduce_add_sync(0xFFFFFFFFu, (int)sum);
     nt_most = __reduce_max_sync(0xFFFFFFFFu, nt_most);
     // CTAs that get a piece: no more than tiles, nor so many that the longest item would be cut into more than STEP_MAX_PARTS
     n_cta = max(1, min((int)gridDim.x, total));

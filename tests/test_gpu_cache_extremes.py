@@ -48,3 +48,24 @@ def test_values_that_round_to_2_to_the_128(ctx, dtype):
         assert np.array_equal(got.view(torch.uint8).cpu().numpy(), want)
     for got, want in ((dc.k_scale, cache.ks), (dc.v_scale, cache.vs)):
         assert np.array_equal(got.cpu().numpy(), want, equal_nan=True)
+
+
+def test_row_offsets_that_make_the_work_too_long_to_count(ctx):
+    """Every other sequence claims all rows again: 2.6e9 tiles of work, more than 31 bits count.  Nothing is done, the status tells."""
+    batch, rows, heads, kv, dim, page, pages = 20000, 4096, 32, 8, 128, 128, 16
+    codes = [torch.zeros((pages, kv, page, dim), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.ones((pages, kv), device=DEV) for _ in range(2)]
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).repeat(batch, 1)
+    dc = binding.PagedCache(*codes, *scales, table, torch.full((batch,), page * pages, dtype=torch.int32, device=DEV))
+    q = torch.ones((rows, heads, dim), dtype=torch.bfloat16, device=DEV)
+    out = torch.full_like(q, 7.0)
+    cu = torch.zeros(batch + 1, dtype=torch.int32, device=DEV)
+    cu[1::2] = rows
+    ctx.ficoco_profile(True)
+    ctx.ficoco_cache_attention(dc, q, cu, out=out)
+    assert ctx.ficoco_status() == 16 and bool((out == 7.0).all())
+    assert [name for name, _, _ in ctx.ficoco_profile_read()] == ["k_cache_step"]
+    ctx.ficoco_profile(False)
+    cu[2:] = rows                                        # one sequence with all rows, the rest with none
+    ctx.ficoco_cache_attention(dc, q, cu, out=out)
+    assert ctx.ficoco_status() == 0 and bool((out == 0.0).all())
