@@ -407,7 +407,7 @@ int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, i
  *
  * Supported: page_size 16, 32, 64 or 128; max_pages * page_size up to 2^30; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
  * multiple of kv_heads, rows * heads below 2^31 (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a
- * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned.  Anything else returns
+ * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned, all other pointers 4-byte aligned.  Anything else returns
  * FICOCO_ERR_INVALID_ARG or FICOCO_ERR_UNSUPPORTED and launches nothing.
  *
  * Attention and weights wait inside their kernels (bounded, status bit 2): after a wait that ran out, calls of these two do nothing until

@@ -38,6 +38,7 @@ cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, 
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y + nb && y < x + na;
@@ -48,6 +49,7 @@ int check_cache(const ficoco_cache* c, CacheView* v) {
   if (c->n_pages < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->batch < 1 || c->max_pages < 1) return FICOCO_ERR_INVALID_ARG;
   if (c->table_stride < c->max_pages) return FICOCO_ERR_INVALID_ARG;
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return FICOCO_ERR_INVALID_ARG;
+  if (!aligned4(c->k_scale) || !aligned4(c->v_scale) || !aligned4(c->page_table) || !aligned4(c->lengths)) return FICOCO_ERR_INVALID_ARG;
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return FICOCO_ERR_UNSUPPORTED;
   if (c->head_dim % 16 != 0 || c->head_dim > 256 || c->kv_heads > 1024 || c->batch > 65535) return FICOCO_ERR_UNSUPPORTED;
   if ((long long)c->n_pages * c->kv_heads * c->page_size > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;   // rows of a tensor map
@@ -69,7 +71,7 @@ int check_rows(const void* p, int rows, long long stride, int dtype, long long r
 }
 
 int check_attention(const ficoco_cache* c, const ficoco_attention_args* a) {
-  if (!a || !a->cu_rows || a->heads < 1) return FICOCO_ERR_INVALID_ARG;
+  if (!a || !a->cu_rows || !aligned4(a->cu_rows) || !aligned4(a->lse) || a->heads < 1) return FICOCO_ERR_INVALID_ARG;
   const int rc = check_rows(a->q, a->rows, a->q_stride, a->dtype, (long long)a->heads * c->head_dim);
   if (rc) return rc;
   if (a->heads % c->kv_heads != 0 || a->window < 0 || a->sinks < 0) return FICOCO_ERR_INVALID_ARG;
@@ -216,7 +218,7 @@ extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, c
   CacheView c;
   int rc = check_cache(cache, &c);
   if (rc) return rc;
-  if (!a->cu_rows) return FICOCO_ERR_INVALID_ARG;
+  if (!a->cu_rows || !aligned4(a->cu_rows)) return FICOCO_ERR_INVALID_ARG;
   const long long width = (long long)c.kv * c.dim;
   if ((rc = check_rows(a->k, a->rows, a->k_stride, a->dtype, width)) || (rc = check_rows(a->v, a->rows, a->v_stride, a->dtype, width))) return rc;
   const CtxAccess x = ctx_access(ctx);
@@ -245,7 +247,7 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   if (a->rows > 0 && overlap(a->out, a->rows * width * es, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es))
     return FICOCO_ERR_INVALID_ARG;
   const size_t lse_bytes = (size_t)a->rows * a->heads * 4;
-  if (a->rows > 0 && a->lse && (((uintptr_t)a->lse & 3) || overlap(a->lse, lse_bytes, a->out, a->rows * width * es) ||
+  if (a->rows > 0 && a->lse && (overlap(a->lse, lse_bytes, a->out, a->rows * width * es) ||
                                 overlap(a->lse, lse_bytes, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es)))
     return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
@@ -278,7 +280,7 @@ extern "C" int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, 
   CacheView c;
   int rc = check_cache(cache, &c);
   if (rc || (rc = check_attention(cache, a))) return rc;
-  if ((a->rows > 0 && !a->lse) || !weights || ((uintptr_t)weights & 3) || n_text < 1 || first < 0 || count < 1) return FICOCO_ERR_INVALID_ARG;
+  if ((a->rows > 0 && !a->lse) || !weights || !aligned4(weights) || n_text < 1 || first < 0 || count < 1) return FICOCO_ERR_INVALID_ARG;
   if ((long long)c.batch * n_text > INT32_MAX || (long long)first + count > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -310,7 +312,7 @@ extern "C" int ficoco_cache_copy(ficoco_ctx* ctx, const ficoco_cache* cache, con
   CacheView c;
   const int rc = check_cache(cache, &c);
   if (rc) return rc;
-  if (n < 0 || (n > 0 && (!src || !dst || src == dst))) return FICOCO_ERR_INVALID_ARG;
+  if (n < 0 || (n > 0 && (!src || !dst || src == dst || !aligned4(src) || !aligned4(dst)))) return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
@@ -333,6 +335,7 @@ extern "C" int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, 
   if (!a->to_table || !a->cu_kept || a->n_kept < 0 || (a->n_kept > 0 && !a->kept) || a->first < 0 || a->to_pages < 1 ||
       a->to_stride < a->to_pages || a->to_table == c.table || a->lengths_out == c.len)
     return FICOCO_ERR_INVALID_ARG;
+  if (!aligned4(a->to_table) || !aligned4(a->kept) || !aligned4(a->cu_kept) || !aligned4(a->lengths_out)) return FICOCO_ERR_INVALID_ARG;
   if ((long long)a->n_kept + (long long)c.batch * a->first > INT32_MAX / 2) return FICOCO_ERR_UNSUPPORTED;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;

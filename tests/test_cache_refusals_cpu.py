@@ -1,10 +1,12 @@
-"""Refusals of the 8-bit cache's calls, without a GPU: tensors that lie on another device than the cache."""
+"""Refusals of the 8-bit cache's calls, without a GPU: tensors that lie on another device than the cache, pointers that a kernel
+could not follow."""
 import types
 
 import pytest
 import torch
 
-from paper_2411_17686_b200 import binding
+from paper_2411_17686_b200 import binding, build
+from tests import test_cache_cpu as A
 
 GPU, OTHER, CPU = torch.device("cuda", 0), torch.device("cuda", 1), torch.device("cpu")
 
@@ -87,3 +89,34 @@ def test_tensors_on_another_device_are_refused(ctx, call, name, device):
         run(ctx, tensors())
     with pytest.raises(ValueError):
         run(ctx, tensors(**{name: device}))
+
+
+# ---- the C entry points, with a context that none may touch (tests/test_cache_cpu.py) ---------------------------------------------
+P = A.P16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.load_library()
+
+
+@pytest.mark.parametrize("by", [1, 2, 3])
+def test_misaligned_pointers_are_refused(lib, by):
+    for name, at in (("k_scale", 3), ("v_scale", 4), ("page_table", 5), ("lengths", 6)):
+        c = A.cache(**{name: P * at + by})
+        assert lib.ficoco_cache_append(A.FAKE, c, A.append(), None) == -1, name
+        assert lib.ficoco_cache_attention(A.FAKE, c, A.attention(), None) == -1, name
+        assert lib.ficoco_cache_weights(A.FAKE, c, A.attention(), 2, 0, 3, P * 4000, None) == -1, name
+        assert lib.ficoco_cache_copy(A.FAKE, c, P * 15, P * 16, 3, None) == -1, name
+        assert lib.ficoco_cache_compact(A.FAKE, c, A.compact(), None) == -1, name
+    c = A.cache()
+    for name, at in (("cu_rows", 8), ("lse", 3000)):
+        a = A.attention(**{name: P * at + by})
+        assert lib.ficoco_cache_attention(A.FAKE, c, a, None) == -1, name
+        assert lib.ficoco_cache_weights(A.FAKE, c, a, 2, 0, 3, P * 4000, None) == -1, name
+    assert lib.ficoco_cache_append(A.FAKE, c, A.append(cu_rows=P * 8 + by), None) == -1
+    assert lib.ficoco_cache_copy(A.FAKE, c, P * 15 + by, P * 16, 3, None) == -1
+    assert lib.ficoco_cache_copy(A.FAKE, c, P * 15, P * 16 + by, 3, None) == -1
+    for name, at in (("to_table", 11), ("kept", 12), ("cu_kept", 13), ("lengths_out", 14)):
+        assert lib.ficoco_cache_compact(A.FAKE, c, A.compact(**{name: P * at + by}), None) == -1, name
