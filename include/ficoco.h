@@ -407,8 +407,9 @@ int ficoco_vision_redundancy_noalloc(const void* tokens, int dtype, int batch, i
  *
  * Supported: page_size 16, 32, 64 or 128; max_pages * page_size up to 2^30; head_dim a multiple of 16 up to 256 (64 and 128 use the tensor cores); heads a
  * multiple of kv_heads, rows * heads below 2^31 (query head h reads key/value head h / (heads / kv_heads)); fp32 or bf16 rows, 16-byte aligned, with a
- * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned, all other pointers 4-byte aligned.  Anything else returns
- * FICOCO_ERR_INVALID_ARG or FICOCO_ERR_UNSUPPORTED and launches nothing.
+ * row stride in elements that is a multiple of 16 bytes; code arrays 16-byte aligned, all other pointers 4-byte aligned; what a call
+ * writes overlaps neither what it reads nor, in an attention call, each other.  Anything else returns FICOCO_ERR_INVALID_ARG or
+ * FICOCO_ERR_UNSUPPORTED and launches nothing.
  *
  * Attention and weights wait inside their kernels (bounded, status bit 2): after a wait that ran out, calls of these two do nothing until
  * ficoco_status has read the word.  Append, copy and compact wait for nothing and go on.
@@ -461,7 +462,6 @@ int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, const ficoco
  * 2^-24 and 2^-38; fp16 to 2^-11 and to 2^-20 of the largest one of its 128 tokens 128 i .. 128 i + 127 (2^-48 of the row's largest, if
  * that is more).  Two terms hold a bf16 query element exactly down to 2^-13 of its row's largest one, where a call has many rows down to
  * 2^-9, and smaller ones to 2^-21 and 2^-17 of that.  Value codes must not be NaN (append writes none).
- * out, lse and q must not overlap.
  */
 enum ficoco_attention_flags { FICOCO_CAUSAL = 1u };
 typedef struct ficoco_attention_args {

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <functional>
+#include <initializer_list>
 #include <new>
 #include <queue>
 #include <vector>
@@ -39,9 +40,20 @@ cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, 
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
+// Bytes that a call reads or writes (p NULL: none).
+struct Span {
+  const void* p;
+  size_t n;
+};
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + b.n && y < x + a.n;
+}
+bool overlap(std::initializer_list<Span> a, std::initializer_list<Span> b) {
+  for (const Span& x : a)
+    for (const Span& y : b)
+      if (overlap(x, y)) return true;
+  return false;
 }
 
 int check_cache(const ficoco_cache* c, CacheView* v) {
@@ -69,6 +81,15 @@ int check_rows(const void* p, int rows, long long stride, int dtype, long long r
   const int es = dtype == FICOCO_BF16 ? 2 : 4;
   return stride * es % 16 == 0 ? FICOCO_OK : FICOCO_ERR_INVALID_ARG;
 }
+
+// The parts of a cache; rows of a call, row offsets and index lists.
+Span codes_of(const ficoco_cache* c, const void* codes) { return {codes, (size_t)c->n_pages * c->kv_heads * c->page_size * c->head_dim}; }
+Span scales_of(const ficoco_cache* c, const float* scales) { return {scales, (size_t)c->n_pages * c->kv_heads * 4}; }
+Span table_of(const ficoco_cache* c) { return {c->page_table, ((size_t)(c->batch - 1) * c->table_stride + c->max_pages) * 4}; }
+Span rows_of(const void* p, int rows, long long stride, size_t width, int dtype) {
+  return {rows > 0 ? p : nullptr, ((size_t)std::max(rows - 1, 0) * stride + width) * (dtype == FICOCO_BF16 ? 2 : 4)};
+}
+Span ints_of(const int* p, size_t n) { return {p, n * 4}; }
 
 int check_attention(const ficoco_cache* c, const ficoco_attention_args* a) {
   if (!a || !a->cu_rows || !aligned4(a->cu_rows) || !aligned4(a->lse) || a->heads < 1) return FICOCO_ERR_INVALID_ARG;
@@ -221,6 +242,10 @@ extern "C" int ficoco_cache_append(ficoco_ctx* ctx, const ficoco_cache* cache, c
   if (!a->cu_rows || !aligned4(a->cu_rows)) return FICOCO_ERR_INVALID_ARG;
   const long long width = (long long)c.kv * c.dim;
   if ((rc = check_rows(a->k, a->rows, a->k_stride, a->dtype, width)) || (rc = check_rows(a->v, a->rows, a->v_stride, a->dtype, width))) return rc;
+  if (overlap({codes_of(cache, cache->k_codes), codes_of(cache, cache->v_codes), scales_of(cache, cache->k_scale), scales_of(cache, cache->v_scale)},
+              {rows_of(a->k, a->rows, a->k_stride, width, a->dtype), rows_of(a->v, a->rows, a->v_stride, width, a->dtype), table_of(cache),
+               ints_of(cache->lengths, c.batch), ints_of(a->cu_rows, c.batch + 1)}))
+    return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
@@ -243,12 +268,12 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   int rc = check_cache(cache, &c);
   if (rc || (rc = check_attention(cache, a))) return rc;
   if ((a->rows > 0 && !a->out) || !aligned16(a->out)) return FICOCO_ERR_INVALID_ARG;
-  const size_t es = a->dtype == FICOCO_BF16 ? 2 : 4, width = (size_t)a->heads * c.dim;
-  if (a->rows > 0 && overlap(a->out, a->rows * width * es, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es))
-    return FICOCO_ERR_INVALID_ARG;
-  const size_t lse_bytes = (size_t)a->rows * a->heads * 4;
-  if (a->rows > 0 && a->lse && (overlap(a->lse, lse_bytes, a->out, a->rows * width * es) ||
-                                overlap(a->lse, lse_bytes, a->q, ((size_t)(a->rows - 1) * a->q_stride + width) * es)))
+  const size_t width = (size_t)a->heads * c.dim;
+  const Span q = rows_of(a->q, a->rows, a->q_stride, width, a->dtype), out = rows_of(a->out, a->rows, width, width, a->dtype);
+  const Span lse = {a->rows > 0 ? a->lse : nullptr, (size_t)a->rows * a->heads * 4};
+  if (overlap({out, lse}, {q, codes_of(cache, cache->k_codes), codes_of(cache, cache->v_codes), scales_of(cache, cache->k_scale),
+                           scales_of(cache, cache->v_scale), table_of(cache), ints_of(cache->lengths, c.batch), ints_of(a->cu_rows, c.batch + 1)}) ||
+      overlap(out, lse))
     return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -282,6 +307,12 @@ extern "C" int ficoco_cache_weights(ficoco_ctx* ctx, const ficoco_cache* cache, 
   if (rc || (rc = check_attention(cache, a))) return rc;
   if ((a->rows > 0 && !a->lse) || !weights || !aligned4(weights) || n_text < 1 || first < 0 || count < 1) return FICOCO_ERR_INVALID_ARG;
   if ((long long)c.batch * n_text > INT32_MAX || (long long)first + count > INT32_MAX) return FICOCO_ERR_UNSUPPORTED;
+  const double bytes = 4.0 * c.batch * a->heads * n_text * count;
+  if (overlap({Span{weights, (size_t)std::min(bytes, 1e18)}},
+              {rows_of(a->q, a->rows, a->q_stride, (size_t)a->heads * c.dim, a->dtype), Span{a->rows > 0 ? a->lse : nullptr, (size_t)a->rows * a->heads * 4},
+               codes_of(cache, cache->k_codes), scales_of(cache, cache->k_scale), table_of(cache), ints_of(cache->lengths, c.batch),
+               ints_of(a->cu_rows, c.batch + 1)}))
+    return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
@@ -313,6 +344,9 @@ extern "C" int ficoco_cache_copy(ficoco_ctx* ctx, const ficoco_cache* cache, con
   const int rc = check_cache(cache, &c);
   if (rc) return rc;
   if (n < 0 || (n > 0 && (!src || !dst || src == dst || !aligned4(src) || !aligned4(dst)))) return FICOCO_ERR_INVALID_ARG;
+  if (n > 0 && overlap({codes_of(cache, cache->k_codes), codes_of(cache, cache->v_codes), scales_of(cache, cache->k_scale),
+                        scales_of(cache, cache->v_scale)}, {ints_of(src, n), ints_of(dst, n)}))
+    return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));
@@ -337,6 +371,14 @@ extern "C" int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* cache, 
     return FICOCO_ERR_INVALID_ARG;
   if (!aligned4(a->to_table) || !aligned4(a->kept) || !aligned4(a->cu_kept) || !aligned4(a->lengths_out)) return FICOCO_ERR_INVALID_ARG;
   if ((long long)a->n_kept + (long long)c.batch * a->first > INT32_MAX / 2) return FICOCO_ERR_UNSUPPORTED;
+  const Span lengths_out = ints_of(a->lengths_out, c.batch);
+  if (overlap({codes_of(cache, cache->k_codes), codes_of(cache, cache->v_codes), scales_of(cache, cache->k_scale), scales_of(cache, cache->v_scale),
+               lengths_out},
+              {Span{a->to_table, ((size_t)(c.batch - 1) * a->to_stride + a->to_pages) * 4}, ints_of(a->n_kept > 0 ? a->kept : nullptr, a->n_kept),
+               ints_of(a->cu_kept, c.batch + 1), table_of(cache), ints_of(cache->lengths, c.batch)}) ||
+      overlap({lengths_out}, {codes_of(cache, cache->k_codes), codes_of(cache, cache->v_codes), scales_of(cache, cache->k_scale),
+                              scales_of(cache, cache->v_scale)}))
+    return FICOCO_ERR_INVALID_ARG;
   const CtxAccess x = ctx_access(ctx);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   CACHE_TRY(ctx, cudaSetDevice(x.device));

@@ -120,3 +120,27 @@ def test_misaligned_pointers_are_refused(lib, by):
     assert lib.ficoco_cache_copy(A.FAKE, c, P * 15, P * 16 + by, 3, None) == -1
     for name, at in (("to_table", 11), ("kept", 12), ("cu_kept", 13), ("lengths_out", 14)):
         assert lib.ficoco_cache_compact(A.FAKE, c, A.compact(**{name: P * at + by}), None) == -1, name
+
+
+def test_outputs_that_overlap_inputs_are_refused(lib):
+    """The library's general rule.  Sizes of tests/test_cache_cpu.py's calls: 10 pages of 2 heads x 64 tokens x 128, 3 sequences, 5 rows."""
+    wide = dict(k_codes=P * 100, v_codes=P * 200, k_scale=P * 300, v_scale=P * 400, page_table=P * 500, lengths=P * 600)
+    c, codes = A.cache(**wide), 10 * 2 * 64 * 128
+    inputs = [P * 100, P * 100 + codes - 16, P * 300, P * 300 + 76, P * 500, P * 500 + 92, P * 600 + 8, P * 8, P * 8 + 12]
+    for at in inputs + [P * 200 + 1024, P * 400 + 4]:
+        assert lib.ficoco_cache_attention(A.FAKE, c, A.attention(lse=at), None) == -1, hex(at)
+        if at % 16 == 0:
+            assert lib.ficoco_cache_attention(A.FAKE, c, A.attention(out=at), None) == -1, hex(at)
+    size = 3 * 4 * 2 * 3 * 4                             # bytes of the weights
+    for at in inputs + [P * 1000, P * 1000 + (4 * 512 + 512) * 2 - 4, P * 3000, P * 3000 + 76, P * 3000 - size + 4]:
+        assert lib.ficoco_cache_weights(A.FAKE, c, A.attention(), 2, 0, 3, at, None) == -1, hex(at)
+    for at in (P * 100, P * 200 + codes - 16, P * 300, P * 400 + 64):
+        assert lib.ficoco_cache_append(A.FAKE, c, A.append(k=at), None) == -1, hex(at)
+        assert lib.ficoco_cache_append(A.FAKE, c, A.append(v=at), None) == -1, hex(at)
+        assert lib.ficoco_cache_append(A.FAKE, c, A.append(cu_rows=at), None) == -1, hex(at)
+        assert lib.ficoco_cache_copy(A.FAKE, c, at, P * 2, 3, None) == -1, hex(at)
+        assert lib.ficoco_cache_copy(A.FAKE, c, P * 2, at, 3, None) == -1, hex(at)
+        for name in ("to_table", "kept", "cu_kept", "lengths_out"):
+            assert lib.ficoco_cache_compact(A.FAKE, c, A.compact(**{name: at}), None) == -1, (name, hex(at))
+    for at in (P * 11, P * 11 + 44, P * 12 + 32, P * 13 + 12, P * 13 - 8, P * 500 + 92, P * 600 + 8):
+        assert lib.ficoco_cache_compact(A.FAKE, c, A.compact(lengths_out=at), None) == -1, hex(at)
