@@ -189,7 +189,8 @@ int attend_prompt(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const
   return FICOCO_OK;
 }
 template <int DIM>
-int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, cudaStream_t st) {
+int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const ficoco_attention_args* a, float scale_log2, bool listed,
+               cudaStream_t st) {
   int* counters;
   float* partials;
   // (also where a prompt needs none: so the first call, whatever its rows, is the one that allocates)
@@ -198,10 +199,12 @@ int attend_dim(ficoco_ctx* ctx, const CtxAccess& x, const CacheView& c, const fi
   if (a->dtype == FICOCO_FP32) return attend_step<float, DIM, 6, 8>(ctx, x, c, a, scale_log2, counters, partials, st);
   const long long rows = (long long)a->rows * (a->heads / c.kv);       // of all sequences, per key/value head
   // The prompt kernel takes 256 rows per CTA and needs about 5000 cycles for a tile of tokens, one CTA per SM; the step kernel takes 16
-  // rows per item, two CTAs per SM, about 3000 cycles a tile: whichever has the shorter line (the tiles per row are the same).
+  // rows per item, two CTAs per SM, about 3000 cycles a tile: whichever has the shorter line (the tiles per row are the same).  Sequences that
+  // open a CTA for less than 256 rows are not counted one by one: their tiles hold 128 rows at most and take less (prompt / step kernel, us: 128
+  // sequences of 40 rows, 640 tokens, 32 heads 558 / 767, with 8 key/value heads 185 / 646; 600 of 12 rows, 32 heads on 8, 593 / 783).
   const long long prompt_ctas = std::max(1ll, rows / PROMPT_ROWS) * c.kv, step_items = (rows / 16 + 1) * c.kv;
   const long long prompt_time = (prompt_ctas + x.num_sms - 1) / x.num_sms * 5000, step_time = step_items * 3000 / (2 * x.num_sms);
-  if (rows > 32ll * c.batch && prompt_time < step_time) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
+  if (!listed || (rows > 32ll * c.batch && prompt_time < step_time)) return attend_prompt<DIM>(ctx, x, c, a, scale_log2, st);
   if (rows <= 8ll * c.batch) return attend_step<__nv_bfloat16, DIM, 2, 8>(ctx, x, c, a, scale_log2, counters, partials, st);
   return attend_step<__nv_bfloat16, DIM, 2, 16>(ctx, x, c, a, scale_log2, counters, partials, st);
 }
@@ -281,10 +284,15 @@ extern "C" int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* cache
   ctx_set_launches(ctx, 0);
   if (a->rows == 0) return FICOCO_OK;
   const float scale_log2 = a->scale * 1.4426950408889634f;
-  // (the tensor-core kernels count tiles of 8 rows by 128 tokens in 32 bits; what could exceed that takes the kernel without tiles)
+  // The step kernel's list of tiles, of 8 rows by 128 tokens, is counted in 32 bits.  What its table's room could make longer takes the kernel
+  // of prompts, which has no list, or, with few rows or fp32, the kernel without tiles (one sequence of 4096 tokens, 32 heads on 8, 64 rows:
+  // 84 us, without tiles 836; 2944 rows: 175 and 22900).
   const double most_tiles = ((double)a->rows * (a->heads / c.kv) / 8 + c.batch) * c.kv * ((double)c.max_pages * c.page / CTILE + 2);
-  if (c.dim == 128 && most_tiles < 2e9) return attend_dim<128>(ctx, x, c, a, scale_log2, st);
-  if (c.dim == 64 && most_tiles < 2e9) return attend_dim<64>(ctx, x, c, a, scale_log2, st);
+  const bool listed = most_tiles < 2e9;
+  if (listed || (a->dtype == FICOCO_BF16 && (long long)a->rows * (a->heads / c.kv) > 32ll * c.batch)) {
+    if (c.dim == 128) return attend_dim<128>(ctx, x, c, a, scale_log2, listed, st);
+    if (c.dim == 64) return attend_dim<64>(ctx, x, c, a, scale_log2, listed, st);
+  }
   const dim3 grid(a->rows, a->heads);
   ctx_prof_tick(ctx, st, "k_cache_attention_simt");
   if (a->dtype == FICOCO_BF16)

@@ -69,3 +69,31 @@ def test_row_offsets_that_make_the_work_too_long_to_count(ctx):
     cu[2:] = rows                                        # one sequence with all rows, the rest with none
     ctx.ficoco_cache_attention(dc, q, cu, out=out)
     assert ctx.ficoco_status() == 0 and bool((out == 0.0).all())
+
+
+@pytest.mark.parametrize("n,heads,kv,dim,dtype,pages,kernel", [
+    (600, 16, 8, 128, "bf16", 1 << 22, "k_cache_prompt"),             # 151 blocks * 8 heads * 2^22 tiles: 5.1e9
+    (70, 32, 32, 64, "bf16", 1 << 23, "k_cache_prompt"),              # 2.6e9
+    (600, 16, 8, 128, "bf16", 1 << 17, "k_cache_prompt"),             # 1.6e8
+    (100, 8, 8, 128, "bf16", 1 << 22, "k_cache_step"),                # 4.5e8
+    (40, 8, 8, 128, "fp32", 1 << 23, "k_cache_step"),                 # 4.0e8
+    (500, 8, 8, 128, "fp32", 1 << 23, "k_cache_attention_simt"),      # 4.3e9
+    (30, 64, 64, 128, "bf16", 1 << 23, "k_cache_attention_simt"),     # 2.6e9, few rows
+])
+def test_tables_with_room_for_very_long_sequences(ctx, n, heads, kv, dim, dtype, pages, kernel):
+    """A table of up to 2^30 tokens, a short sequence: which kernel is taken around the limit of 2e9 tiles, and its result."""
+    rng = np.random.default_rng(n)
+    cache = R.Cache(rng, [700], 128, kv, dim)
+    d = cache.device()
+    table = torch.full((1, pages), -7, dtype=torch.int32, device=DEV)
+    table[:, :d.page_table.shape[1]] = d.page_table
+    dc = binding.PagedCache(d.k_codes, d.v_codes, d.k_scale, d.v_scale, table, d.lengths)
+    q = torch.from_numpy(rng.standard_normal((n, heads, dim)) * 1.5).to(dict(bf16=torch.bfloat16, fp32=torch.float32)[dtype]).to(DEV)
+    ctx.ficoco_profile(True)
+    out, lse = ctx.ficoco_cache_attention(dc, q, R.cu([n]), want_lse=True)
+    assert [name for name, _, _ in ctx.ficoco_profile_read()] == [kernel]
+    ctx.ficoco_profile(False)
+    assert ctx.ficoco_status() == 0
+    want, want_lse, tol, ltol = R.attention(cache, q, [n])
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+    assert (np.abs(lse.double().cpu().numpy() - want_lse) <= ltol).all()
