@@ -347,6 +347,13 @@ class PagePool:
         return out[:n].tolist(), (None if src.value < 0 else (src.value, dst.value))
 
 
+def _c_ints(**values: int) -> None:
+    """Refuses what a C int does not hold (ctypes would cut it to its low 32 bits)."""
+    for name, x in values.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise ValueError(f"{name} = {x} is no 32-bit integer")
+
+
 def _int32(name: str, t, n: Optional[int] = None, device=None) -> int:
     """Address of a contiguous cuda int32 tensor, on ``device`` if one is given."""
     if t.dtype is not _load_torch().int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n) or \
@@ -632,6 +639,8 @@ class Context:
         cs = cache.struct
         self._same_device(cache, q)
         stride = _rows3("q", q, cs.head_dim)
+        if window or sinks:
+            _c_ints(window=window, sinks=sinks)
         return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1, cache.device), None, None, stride,
                                      cache.scale if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
                                      window, sinks, FICOCO_CAUSAL if causal else 0)
@@ -671,6 +680,7 @@ class Context:
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != cache.device:
             raise ValueError("lse must be contiguous fp32 [rows, heads] on q's device")
+        _c_ints(n_text=n_text, first=first, count=count)
         shape = (cache.struct.batch, q.shape[1], n_text, count)
         if out is None:
             out = _new(q, shape, torch.float32)
@@ -699,6 +709,7 @@ class Context:
         torch = _load_torch()
         cs = cache.struct
         self._same_device(cache, to_table)
+        _c_ints(first=first)
         if to_table.dtype != torch.int32 or to_table.dim() != 2 or to_table.shape[0] != cs.batch or not to_table.is_cuda or \
                 to_table.stride(1) != 1:
             raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")

@@ -91,6 +91,22 @@ def test_tensors_on_another_device_are_refused(ctx, call, name, device):
         run(ctx, tensors(**{name: device}))
 
 
+def test_numbers_that_no_c_int_holds_are_refused(ctx):
+    """Their low 32 bits would be a window of 5, token 0, ..."""
+    t = tensors()
+    for over in (dict(window=(1 << 32) + 5), dict(window=1 << 31), dict(window=8, sinks=(1 << 32) + 1), dict(sinks=-(1 << 33))):
+        with pytest.raises(ValueError):
+            ctx.ficoco_cache_attention(cache(), t.q, t.cu, out=t.out, lse=t.lse, stream=0, **over)
+        with pytest.raises(ValueError):
+            ctx.ficoco_cache_weights(cache(), t.q, t.lse, t.cu, TEXT, 0, COUNT, out=t.weights, stream=0, **over)
+    with pytest.raises(ValueError):
+        ctx.ficoco_cache_weights(cache(), t.q, t.lse, t.cu, TEXT, 1 << 32, COUNT, out=t.weights, stream=0)
+    with pytest.raises(ValueError):
+        ctx.ficoco_cache_compact(cache(), t.to, t.kept, t.cu, first=1 << 32, lengths=t.lengths, stream=0)
+    with pytest.raises(Reached):
+        ctx.ficoco_cache_attention(cache(), t.q, t.cu, out=t.out, lse=t.lse, stream=0, window=(1 << 31) - 1, sinks=(1 << 31) - 1)
+
+
 # ---- the C entry points, with a context that none may touch (tests/test_cache_cpu.py) ---------------------------------------------
 P = A.P16
 
