@@ -639,7 +639,7 @@ class Context:
         cs = cache.struct
         self._same_device(cache, q)
         stride = _rows3("q", q, cs.head_dim)
-        if window or sinks:
+        if (window | sinks) >> 31:
             _c_ints(window=window, sinks=sinks)
         return ficoco_attention_args(q.data_ptr(), _int32("cu_rows", cu_rows, cs.batch + 1, cache.device), None, None, stride,
                                      cache.scale if scale is None else scale, _dtype_code(q), q.shape[0], q.shape[1],
@@ -680,7 +680,8 @@ class Context:
         a = self._attention_args(cache, q, cu_rows, scale, causal, window, sinks)
         if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != cache.device:
             raise ValueError("lse must be contiguous fp32 [rows, heads] on q's device")
-        _c_ints(n_text=n_text, first=first, count=count)
+        if (n_text | first | count) >> 31:
+            _c_ints(n_text=n_text, first=first, count=count)
         shape = (cache.struct.batch, q.shape[1], n_text, count)
         if out is None:
             out = _new(q, shape, torch.float32)
@@ -709,7 +710,8 @@ class Context:
         torch = _load_torch()
         cs = cache.struct
         self._same_device(cache, to_table)
-        _c_ints(first=first)
+        if first >> 31:
+            _c_ints(first=first)
         if to_table.dtype != torch.int32 or to_table.dim() != 2 or to_table.shape[0] != cs.batch or not to_table.is_cuda or \
                 to_table.stride(1) != 1:
             raise ValueError(f"to_table must be a cuda int32 tensor [{cs.batch}, pages]")

@@ -97,3 +97,28 @@ def test_tables_with_room_for_very_long_sequences(ctx, n, heads, kv, dim, dtype,
     want, want_lse, tol, ltol = R.attention(cache, q, [n])
     assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
     assert (np.abs(lse.double().cpu().numpy() - want_lse) <= ltol).all()
+
+
+@pytest.mark.parametrize("n_text,dim,dtype,kernel", [
+    (60000, 128, "bf16", "k_cache_weights"),              # (n_text * group + 64) * n_text: 3.6e9
+    (70000, 128, "bf16", "k_cache_weights_simt"),         # 4.9e9: beyond 32 bits
+    (5, 64, "fp32", "k_cache_weights"),
+    (5, 80, "fp32", "k_cache_weights_simt"),
+])
+def test_weights_of_more_text_rows_than_there_are(ctx, n_text, dim, dtype, kernel):
+    """Which kernel is taken around the limit of 32-bit row numbers, and its result: rows that are not there weigh nothing."""
+    rng = np.random.default_rng(n_text)
+    rows, heads, kv, first, count = [90, 3], 2, 2, 4, 50
+    cache = R.Cache(rng, [120, 40], 32, kv, dim)
+    q = torch.from_numpy(rng.standard_normal((sum(rows), heads, dim))).to(dict(bf16=torch.bfloat16, fp32=torch.float32)[dtype]).to(DEV)
+    dc = cache.device()
+    _, lse = ctx.ficoco_cache_attention(dc, q, R.cu(rows), want_lse=True)
+    out = torch.full((2, heads, n_text, count), float("nan"), device=DEV)
+    ctx.ficoco_profile(True)
+    ctx.ficoco_cache_weights(dc, q, lse, R.cu(rows), n_text, first, count, out=out)
+    assert [name for name, _, _ in ctx.ficoco_profile_read()] == [kernel]
+    ctx.ficoco_profile(False)
+    assert ctx.ficoco_status() == 0
+    want, tol = R.weights(cache, q, lse, rows, n_text, first, count)
+    got = out.double().cpu().numpy()
+    assert (np.abs(got - want) <= tol).all() and (got[want == 0] == 0).all()
