@@ -7,8 +7,9 @@
 // lengths on the device; the host sizes the grid for the most pages that so many rows can touch (rows / page + 2 per sequence), the
 // CTAs beyond return at once.
 // What bounds them: instruction issue and HBM on prompts, the chain of lookups (sequence, length, page, old scale) on single tokens.
-// Measured: append of 16 prompts of 640 rows, 32 heads of 128, bf16, 53 us, 4.7 TB/s; one row of 64 sequences 4.2 us; compact of 48
-// sequences in pages of 16, 32 heads, 153 us, 4.1 TB/s; copy of 190 pages of 128 tokens and 8 heads 20.6 us, 4.8 TB/s.
+// Measured, replayed from a graph: append of 16 prompts of 640 rows, 32 heads of 128, bf16, 55 us, 4.5 TB/s, fp32 76 us; one row of 64 sequences
+// 4.2 us (6.9 called from Python one after the other, which is the host's time); compact of 48 sequences in pages of 16, 32 heads, 151 us, 4.1
+// TB/s; copy of 190 pages of 128 tokens and 8 heads 20.6 us, 4.8 TB/s (17.8 called one after the other on one pool, whose pages stay in L2).
 #pragma once
 #include "cache_common.cuh"
 

@@ -19,9 +19,10 @@
 // its partner exchange maxima), warps 16 and 17 convert values, warp 18 TMA and page scales, warp 19 MMA.  One CTA per SM and work item; a
 // sequence's last rows, which see most, go first.
 //
-// Measured: four causal prompts of 2500 to 2944 rows over up to 4000 tokens, 32 heads of 128: 467 us, 0.68 PFLOP/s of what is seen.  A tile
+// Measured: four causal prompts of 2500 to 2944 rows over up to 4000 tokens, 32 heads of 128: 472 us, 0.67 PFLOP/s of what is seen.  A tile
 // of tokens takes 4800 cycles for both row tiles, its products 2048: the chain scores, weights, products of one row tile (3500
 // cycles of softmax with both tiles' warps on the schedulers) is what is left; with a quarter of the exponentials it would be 376 us.
+// A reference that only rises is 464 us.
 #pragma once
 #include "cache_umma.cuh"
 

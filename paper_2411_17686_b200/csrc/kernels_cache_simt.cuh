@@ -3,7 +3,8 @@
 // A thread takes a token: its key's codes are read 16 at a time and multiplied with the query row, which lies in shared memory
 // as fp32.  For the output a thread takes one or two dimensions and walks the tokens of the chunk.  What bounds it is arithmetic (a
 // conversion and a multiplication per code and query row): the tensor-core kernels take head sizes of 64 and 128.  Measured where both can
-// run: 64 ragged sequences of 64 to 8192 tokens, 32 heads on 8 of 128, 741 us (62 there); weights of 16 sequences 677 us (35).
+// run: 64 ragged sequences of 64 to 8192 tokens, 32 heads on 8 of 128, 741 us (65 there); weights of 16 sequences 677 us (36).  Heads of 96: 683
+// and 268 us, of 256: 925 us.
 #pragma once
 #include "cache_common.cuh"
 

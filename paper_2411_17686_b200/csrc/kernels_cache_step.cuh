@@ -23,9 +23,10 @@
 // page scales, warp 9 MMA.  Tile i's scores are computed while tile i - 1's weights are multiplied; keys are given back as
 // soon as the scores exist; queries are two items ahead, page indexes two and scales one batch of 32 / (pages per tile) tiles.
 //
-// Measured (bf16, heads of 128): 32 sequences of 4096 tokens and 8 heads 54 us, 5.0 TB/s; 64 ragged ones of 64 to 8192 tokens 62 us, 3.4
-// TB/s; a window of 8000 tokens of 8 sequences 37 us; one sequence of 640 tokens and 32 heads 12.4 us; one tile 8.4 us, which is what start
-// and end of a CTA take.  fp32 rows, one sequence of 65536 tokens: 55 us, 2.4 TB/s.
+// Measured (bf16, heads of 128, replayed from a graph): 32 sequences of 4096 tokens and 8 heads 56 us, 4.8 TB/s; 64 ragged ones of 64 to 8192
+// tokens 65 us, 3.3 TB/s; a window of 8000 tokens of 8 sequences 38 us; one sequence of 640 tokens and 32 heads 12.4 us; one tile 8.6 us, which
+// is what start and end of a CTA take.  fp32 rows, one sequence of 65536 tokens: 54 us, 2.5 TB/s (45 with a maximum common to the four softmax
+// warps, which costs bf16 rows a barrier per tile).
 #pragma once
 #include <float.h>
 #include "cache_umma.cuh"

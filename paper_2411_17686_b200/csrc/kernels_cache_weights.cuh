@@ -11,7 +11,7 @@
 // Roles: warps 0-3 and 4-7 output, every other tile each (thread = token), warps 8-11 queries, warp 12 TMA and key scales, warp 13
 // MMA.
 //
-// Measured: 16 sequences, 64 text rows over 576 tokens, 32 heads, bf16 (75 MB of results, 38 MB of keys): 35 us; the stores alone 16.5.  One
+// Measured: 16 sequences, 64 text rows over 576 tokens, 32 heads, bf16 (75 MB of results, 38 MB of keys): 36 us; the stores alone 16.5.  One
 // sequence of 37 over 2880, fp32, 32 heads on 8: 14.4 us.
 #pragma once
 #include "cache_umma.cuh"
